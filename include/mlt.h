@@ -17,8 +17,9 @@
  *     rounded to `dtype` with round-to-nearest-even.
  *   - Return value: MLT_OK or a negative mlt_status. No C++ exception crosses the boundary and
  *     nothing aborts. On an error nothing has been enqueued.
+ *     The 8-bit operators say themselves which of their tensors are e4m3 or fp32.
  *   - Device memory of the library's own: the GEMM entry points (few tiles against a long K),
- *     mlt_paged_attn_decode (few sequences x heads) and mlt_mha_fwd (few query tiles against many
+ *     mlt_paged_attn_decode and its 8-bit form (few sequences x heads) and mlt_mha_fwd (few query tiles against many
  *     keys) may spread one result over several workgroups and then keep fp32 partial results in a
  *     scratch buffer, one per (device, stream), allocated with hipMalloc at the first call that
  *     needs it, grown by doubling from 4 MiB (32 MiB covers every split the library chooses by
@@ -173,6 +174,98 @@ int mlt_paged_attn_decode(int64_t B, int64_t H, int64_t D, int64_t block_size, i
                           int64_t num_blocks, const void* Q, const void* Kc, const void* Vc,
                           const int32_t* block_table, const int32_t* seq_lens, void* O,
                           float scale, int dtype, void* stream);
+
+/*
+ * ---- 8 bits: weights and activations for mlt_gemm_fp8, and a paged cache of half the size.
+ * e4m3 is the OCP format (1 sign, 4 exponent and 3 mantissa bits, largest value 448, NaN but no infinities), one byte an
+ * element. A number is its e4m3 value times the fp32 scale of its block. The scales that the library writes are powers of
+ * two: the smallest s >= 2^-100 with max |x| <= 448 s over the block's finite x, so that the rounding to e4m3 (to nearest, ties to
+ * even) is the only one. Infinities and NaN become NaN. The scales that it reads may be any positive finite numbers (from 2^-100 up).
+ */
+
+/*
+ * Quantisation of a matrix to e4m3, with a scale for each block of 128 columns by block_rows rows: 1 (the rows of an activation)
+ * or 128 (a weight).
+ *   X       device, M x K row-major of `dtype`, row stride ldx >= K elements
+ *   Xq      device, M x K row-major e4m3, row stride ldq >= K; written
+ *   S       device, fp32 [ceil(K / 128)][ceil(M / block_rows)], row stride lds >= ceil(M / block_rows); written. The last
+ *           block of a row or a column may be smaller.
+ * K, ldx multiples of 8 and (with more than one row) ldq of 16, X and Xq 16-byte and S 4-byte aligned (else MLT_ERR_UNSUPPORTED for the sizes, MLT_ERR_INVALID_ARG for the
+ * pointers); other block_rows: MLT_ERR_UNSUPPORTED. M or K equal to 0 is a no-op.
+ */
+int mlt_quant_fp8(int64_t M, int64_t K, const void* X, int64_t ldx, int64_t block_rows, void* Xq, int64_t ldq, float* S,
+                  int64_t lds, int dtype, void* stream);
+
+/*
+ * The matrix product of e4m3 operands with block scales, C = A * B^T with B stored N x K:
+ *   C[m][n] = sum over kb of Sa[kb][m] * Sb[kb][n / 128] * sum over k = 128 kb .. 128 kb + 127 of A[m][k] * B[n][k]
+ * The sum over a block and the sum over the blocks are fp32; C is rounded once to `dtype`.
+ *   A       device, M x K row-major e4m3, row stride lda >= K
+ *   Sa      device, fp32 [ceil(K / 128)][M], row stride ldsa >= M
+ *   B       device, N x K row-major e4m3, row stride ldb >= K
+ *   Sb      device, fp32 [ceil(K / 128)][ceil(N / 128)], row stride ldsb >= ceil(N / 128)
+ *   C       device, M x N row-major of `dtype` (any alignment of its elements), row stride ldc >= N; written, never read
+ * K, lda and ldb are multiples of 16 (MLT_ERR_UNSUPPORTED otherwise; fill up with zeros), A and B 16-byte, Sa, Sb 4-byte
+ * aligned. M == 0 or N == 0 is a no-op, K == 0 stores zeros. Strides so large that 256 rows span 2^31 bytes:
+ * MLT_ERR_UNSUPPORTED.
+ */
+int mlt_gemm_fp8(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const float* Sa, int64_t ldsa, const void* B,
+                 int64_t ldb, const float* Sb, int64_t ldsb, void* C, int64_t ldc, int dtype, void* stream);
+
+/*
+ * Appending to the cache of mlt_paged_attn_decode: the queries and keys of T new tokens are turned by the angles of their
+ * positions, and the keys and values go to the slots that the block table names.
+ *   Q, K, V      device, `dtype`: T rows of Hq, H and H heads of D elements side by side, row strides ldq, ldk, ldv (elements,
+ *                multiples of 8: parts of one fused projection's result are fine). Hq may be 0 (no queries; Q, Qo unused).
+ *   offsets      device, int32 [B + 1], 0 = offsets[0] <= offsets[1] <= ... <= T: rows offsets[b] .. offsets[b + 1] - 1 are
+ *                the new tokens of sequence b, in order (none, one, many). Rows from offsets[B] on belong to nobody: they are
+ *                not read, and nothing is written for them.
+ *   seq_lens     device, int32 [B]: tokens of each sequence WITH the new ones, as the attention takes them afterwards. The
+ *                i-th new token of sequence b has position seq_lens[b] - (offsets[b + 1] - offsets[b]) + i.
+ *   block_table, Kc, Vc, block_size, max_blocks, num_blocks   as for mlt_paged_attn_decode, H the cache's heads
+ *   cos, sin     device, fp32 [positions][rot / 2]. Of every head of Q and K the leading `rot` elements are turned, in pairs
+ *                (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin) with the row of the token's position: elements i and i + rot / 2,
+ *                or with `interleaved` != 0 elements 2 i and 2 i + 1. Computed in fp32, rounded once. rot = 0: none, cos
+ *                and sin unused.
+ *   Qo           device, contiguous [T, Hq, D]: the turned queries
+ * A token whose position lies outside [0, max_blocks * block_size), or whose block number outside [0, num_blocks), is not written
+ * to the cache; a position outside [0, positions) takes the nearest row of cos and sin. No two tokens may have one
+ * slot. Slots of no new token keep what they hold. D must be 64 or 128, block_size a multiple of 16 up to 1024, rot a multiple of 16 up to D
+ * (MLT_ERR_UNSUPPORTED); all tensors of `dtype` 16-byte aligned (MLT_ERR_INVALID_ARG). T or B equal to 0 is a no-op.
+ */
+int mlt_paged_append(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks,
+                     int64_t num_blocks, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                     const int32_t* offsets, const int32_t* seq_lens, const int32_t* block_table, const float* cos, const float* sin,
+                     int64_t rot, int64_t positions, int interleaved, void* Qo, void* Kc, void* Vc, int dtype, void* stream);
+
+/*
+ * mlt_paged_append into an 8-bit cache:
+ *   Kc, Vc       device, contiguous e4m3 [num_blocks, H, block_size, D]
+ *   Ks, Vs       device, fp32 [num_blocks, H]: the scale of a block's keys (values) of one head
+ * The turned keys are rounded from fp32 to e4m3. A block whose first slot is among the new ones starts afresh: its scale is
+ * that of the new tokens. One that holds earlier tokens of its sequence keeps its scale (raised to a power of two) while it is large enough;
+ * otherwise it takes the new tokens' scale, and the earlier tokens are rounded again in it. All new tokens of a
+ * (block, head) are written by one owner: no two sequences may append to one block in one call. Otherwise as mlt_paged_append.
+ */
+int mlt_paged_append_fp8(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks,
+                         int64_t num_blocks, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                         const int32_t* offsets, const int32_t* seq_lens, const int32_t* block_table, const float* cos,
+                         const float* sin, int64_t rot, int64_t positions, int interleaved, void* Qo, void* Kc, void* Vc, float* Ks,
+                         float* Vs, int dtype, void* stream);
+
+/*
+ * mlt_paged_attn_decode over an 8-bit cache, with Hq / H query heads to each key/value head (query head q reads head
+ * q / (Hq / H)):
+ *   o = sum_j softmax_j(scale * q . k_j) v_j,   j = 0 .. seq_lens[b] - 1,   0 <= seq_lens[b] <= max_blocks * block_size
+ *   Q, O          device, contiguous [B, Hq, D] of `dtype`
+ *   Kc, Vc, Ks, Vs, block_table, block_size, max_blocks, num_blocks   as for mlt_paged_append_fp8
+ * A sequence without keys gives zeros. The weights keep 11 bits whatever `dtype`. Slots behind the last key are read in
+ * units of 16 and ignored, as in mlt_paged_attn_decode, and so are the limits of what is read, the clamping of lengths (here
+ * to 0 from below) and block numbers, and the requirements. H must divide Hq (MLT_ERR_INVALID_ARG).
+ */
+int mlt_paged_attn_decode_fp8(int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks,
+                              int64_t num_blocks, const void* Q, const void* Kc, const void* Vc, const float* Ks, const float* Vs,
+                              const int32_t* block_table, const int32_t* seq_lens, void* O, float scale, int dtype, void* stream);
 
 /* Static, human-readable text for a status code. */
 const char* mlt_status_string(int status);

@@ -21,7 +21,8 @@ MLT_ERR_SCRATCH = -5
 
 # include/mlt.h (the operations) and include/mlt_diag.h (probes, timing hooks, kernel-choice overrides)
 EXPORTS = ("mlt_gemm", "mlt_gemm_noalloc", "mlt_gemm_acc", "mlt_gemm_tiled", "mlt_gemm_bias_act", "mlt_mha_fwd",
-           "mlt_paged_attn_decode", "mlt_status_string", "mlt_version")
+           "mlt_paged_attn_decode", "mlt_quant_fp8", "mlt_gemm_fp8", "mlt_paged_append", "mlt_paged_append_fp8",
+           "mlt_paged_attn_decode_fp8", "mlt_status_string", "mlt_version")
 DIAG_EXPORTS = ("mlt_probe_mfma", "mlt_probe_mfma16", "mlt_probe_hbm_read", "mlt_set_timing_events",
                 "mlt_last_kernel", "mlt_query_tiling", "mlt_diag_force_variant",
                 "mlt_diag_force_k_parts", "mlt_diag_force_key_split", "mlt_diag_set_persistent_grid")
@@ -53,6 +54,16 @@ _lib.mlt_mha_fwd.argtypes = [_i64, _i64, _i64, _i64, _i64, _p, _p, _p, _p, ctype
 _lib.mlt_paged_attn_decode.restype = _i32
 _lib.mlt_paged_attn_decode.argtypes = [_i64, _i64, _i64, _i64, _i64, _i64, _p, _p, _p, _p, _p, _p,
                                        ctypes.c_float, _i32, _p]
+_lib.mlt_quant_fp8.restype = _i32
+_lib.mlt_quant_fp8.argtypes = [_i64, _i64, _p, _i64, _i64, _p, _i64, _p, _i64, _i32, _p]
+_lib.mlt_gemm_fp8.restype = _i32
+_lib.mlt_gemm_fp8.argtypes = [_i64, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _i32, _p]
+_lib.mlt_paged_append.restype = _i32
+_lib.mlt_paged_append.argtypes = [_i64] * 8 + [_p, _i64] * 3 + [_p] * 5 + [_i64, _i64, _i32, _p, _p, _p, _i32, _p]
+_lib.mlt_paged_append_fp8.restype = _i32
+_lib.mlt_paged_append_fp8.argtypes = [_i64] * 8 + [_p, _i64] * 3 + [_p] * 5 + [_i64, _i64, _i32, _p, _p, _p, _p, _p, _i32, _p]
+_lib.mlt_paged_attn_decode_fp8.restype = _i32
+_lib.mlt_paged_attn_decode_fp8.argtypes = [_i64] * 7 + [_p] * 8 + [ctypes.c_float, _i32, _p]
 _lib.mlt_probe_mfma.restype = _i32
 _lib.mlt_probe_mfma.argtypes = [_i32, _p, _p, ctypes.POINTER(ctypes.c_double), _p]
 _lib.mlt_probe_mfma16.restype = _i32
@@ -402,4 +413,198 @@ def mlt_mha_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, scale: float,
                               O.data_ptr(), float(scale), int(causal), dt, _stream(stream, Q.device))
     if rc != MLT_OK:
         raise MltError(rc, "mlt_mha_fwd")
+    return O
+
+
+# ---- 8 bits: tensors of torch.float8_e4m3fn with fp32 scales
+
+E4M3 = torch.float8_e4m3fn
+
+
+def _gpu(name: str, *tensors) -> None:
+    """All of them (None aside) on one GPU."""
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("%s needs GPU tensors" % name)
+        if device is None:
+            device = t.device
+        elif t.device != device:
+            raise ValueError("%s: all tensors must be on one GPU" % name)
+
+
+def _scales(t: torch.Tensor, shape, name: str) -> int:
+    if t.dtype != torch.float32 or tuple(t.shape) != shape:
+        raise ValueError("%s must be an fp32 tensor of shape %s" % (name, list(shape)))
+    return _rows_contiguous(t, name)
+
+
+def mlt_quant_fp8(X: torch.Tensor, block_rows: int = 1, Xq: torch.Tensor | None = None, S: torch.Tensor | None = None, stream=None):
+    """Xq (e4m3 [M, K]) and S (fp32 [ceil(K/128), ceil(M/block_rows)]) of X [M, K]: a power of two as the scale of every
+    block_rows x 128 block. block_rows: 1 (activations) or 128 (weights)."""
+    _gpu("mlt_quant_fp8", X, Xq, S)
+    dt, ldx = _dtype_code(X), _rows_contiguous(X, "X")
+    M, K = X.shape
+    rows = int(block_rows)
+    shape = (-(-K // 128), -(-M // rows) if rows > 0 else 0)
+    if Xq is None:
+        Xq = torch.empty((M, -(-K // 16) * 16), dtype=E4M3, device=X.device)[:, :K]     # rows start on 16 bytes
+    elif Xq.dtype != E4M3 or Xq.shape != X.shape:
+        raise ValueError("Xq must be a float8_e4m3fn tensor of X's shape")
+    if S is None:
+        S = torch.empty(shape, dtype=torch.float32, device=X.device)
+    ldq, lds = _rows_contiguous(Xq, "Xq"), _scales(S, shape, "S")
+    with _OtherDevice(X.device):
+        rc = _lib.mlt_quant_fp8(M, K, X.data_ptr(), ldx, rows, Xq.data_ptr(), ldq, S.data_ptr(), lds, dt, _stream(stream, X.device))
+    if rc != MLT_OK:
+        raise MltError(rc, "mlt_quant_fp8")
+    return Xq, S
+
+
+def mlt_gemm_fp8(A: torch.Tensor, Sa: torch.Tensor, B: torch.Tensor, Sb: torch.Tensor, C: torch.Tensor | None = None,
+                 dtype: torch.dtype = torch.bfloat16, stream=None) -> torch.Tensor:
+    """C = (A * Sa) @ (B * Sb).T: A [M, K], B [N, K] e4m3, Sa [ceil(K/128), M] and Sb [ceil(K/128), ceil(N/128)] fp32, as
+    mlt_quant_fp8 makes them with block_rows 1 and 128. C (`dtype`, where it is not given) is bf16 or fp16 [M, N]."""
+    _gpu("mlt_gemm_fp8", A, Sa, B, Sb, C)
+    if A.dtype != E4M3 or B.dtype != E4M3:
+        raise TypeError("A and B must be float8_e4m3fn tensors")
+    lda, ldb = _rows_contiguous(A, "A"), _rows_contiguous(B, "B")
+    M, K = A.shape
+    N = B.shape[0]
+    if B.shape[1] != K:
+        raise ValueError("inner dimensions differ: %d vs %d" % (K, B.shape[1]))
+    kb = -(-K // 128)
+    ldsa, ldsb = _scales(Sa, (kb, M), "Sa"), _scales(Sb, (kb, -(-N // 128)), "Sb")
+    if C is None:
+        C = torch.empty((M, N), dtype=dtype, device=A.device)
+    elif tuple(C.shape) != (M, N):
+        raise ValueError("C has the wrong shape")
+    dt, ldc = _dtype_code(C), _rows_contiguous(C, "C")
+    with _OtherDevice(A.device):
+        rc = _lib.mlt_gemm_fp8(M, N, K, A.data_ptr(), lda, Sa.data_ptr(), ldsa, B.data_ptr(), ldb, Sb.data_ptr(), ldsb, C.data_ptr(), ldc, dt,
+                               _stream(stream, A.device))
+    if rc != MLT_OK:
+        raise MltError(rc, "mlt_gemm_fp8")
+    return C
+
+
+def _head_rows(t: torch.Tensor, T: int, D: int, dtype, name: str) -> int:
+    """Row stride of [T, heads, D] whose heads lie side by side."""
+    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D or t.dtype != dtype:
+        raise ValueError("%s must be [%d, heads, %d] of K's type" % (name, T, D))
+    if (D > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != D):
+        raise ValueError("%s: the heads of a token must lie side by side" % name)
+    return t.stride(0) if T > 1 else t.shape[1] * D
+
+
+def _append(name: str, Q, K, V, offsets, seq_lens, block_table, cos, sin, Kc, Vc, Ks, Vs, Qo, interleaved, stream):
+    _gpu(name, K, V, Q, offsets, seq_lens, block_table, cos, sin, Kc, Vc, Ks, Vs, Qo)
+    dt = _dtype_code(K)
+    if K.dim() != 3:
+        raise ValueError("%s: K must be [tokens, heads, D]" % name)
+    T, H, D = K.shape
+    ldk, ldv = _head_rows(K, T, D, K.dtype, "K"), _head_rows(V, T, D, K.dtype, "V")
+    if V.shape != K.shape:
+        raise ValueError("%s: K and V differ in shape" % name)
+    Hq, ldq = 0, 0
+    if Q is not None:
+        Hq, ldq = Q.shape[1] if Q.dim() == 3 else 0, _head_rows(Q, T, D, K.dtype, "Q")
+        if Qo is None:
+            Qo = torch.empty((T, Hq, D), dtype=K.dtype, device=K.device)
+        elif Qo.dtype != K.dtype or Qo.shape != Q.shape or not Qo.is_contiguous():
+            raise ValueError("%s: Qo must be contiguous, of Q's shape and type" % name)
+    elif Qo is not None:
+        raise ValueError("%s: Qo without Q" % name)
+    if Kc.dim() != 4 or Kc.shape[1] != H or Kc.shape[3] != D or Vc.shape != Kc.shape:
+        raise ValueError("%s: the cache must be [num_blocks, %d, block_size, %d]" % (name, H, D))
+    want = K.dtype if Ks is None else E4M3
+    if Kc.dtype != want or Vc.dtype != want:
+        raise ValueError("%s: the cache must be of type %s" % (name, want))
+    if block_table.dim() != 2 or seq_lens.dim() != 1:
+        raise ValueError("%s: block_table / seq_lens shape" % name)
+    B = seq_lens.shape[0]
+    if any(t.dtype != torch.int32 for t in (offsets, seq_lens, block_table)):
+        raise ValueError("%s: offsets, seq_lens and block_table must be int32" % name)
+    if tuple(offsets.shape) != (B + 1,) or block_table.shape[0] != B:
+        raise ValueError("%s: offsets / block_table shape" % name)
+    rot, positions = 0, 0
+    if (cos is None) != (sin is None):
+        raise ValueError("%s: cos and sin come together" % name)
+    if cos is not None:
+        if cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32:
+            raise ValueError("%s: cos and sin must be fp32 [positions, rot / 2]" % name)
+        positions, rot = cos.shape[0], 2 * cos.shape[1]
+    for s in (Ks, Vs):
+        if s is not None and (s.dtype != torch.float32 or tuple(s.shape) != (Kc.shape[0], H)):
+            raise ValueError("%s: Ks and Vs must be fp32 [num_blocks, %d]" % (name, H))
+    for t in (offsets, seq_lens, block_table, cos, sin, Kc, Vc, Ks, Vs):
+        if t is not None and not t.is_contiguous():
+            raise ValueError("%s: offsets, seq_lens, block_table, cos, sin and the cache must be contiguous" % name)
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    head = (T, B, Hq, H, D, Kc.shape[2], block_table.shape[1], Kc.shape[0], ptr(Q), ldq, K.data_ptr(), ldk, V.data_ptr(), ldv, offsets.data_ptr(),
+            seq_lens.data_ptr(), block_table.data_ptr(), ptr(cos), ptr(sin), rot, positions, int(bool(interleaved)), ptr(Qo), Kc.data_ptr(), Vc.data_ptr())
+    with _OtherDevice(K.device):
+        at = _stream(stream, K.device)
+        rc = _lib.mlt_paged_append(*head, dt, at) if Ks is None else _lib.mlt_paged_append_fp8(*head, Ks.data_ptr(), Vs.data_ptr(), dt, at)
+    if rc != MLT_OK:
+        raise MltError(rc, name)
+    return Qo
+
+
+def mlt_paged_append(Q: torch.Tensor | None, K: torch.Tensor, V: torch.Tensor, offsets: torch.Tensor, seq_lens: torch.Tensor,
+                     block_table: torch.Tensor, cos: torch.Tensor | None, sin: torch.Tensor | None, Kc: torch.Tensor, Vc: torch.Tensor,
+                     Qo: torch.Tensor | None = None, interleaved: bool = False, stream=None) -> torch.Tensor | None:
+    """The new tokens' keys (turned by their positions' angles) and values into the paged cache, in place; returns the turned
+    queries. Q [T, Hq, D] (or None), K, V [T, H, D]: a token's heads side by side, any row stride; offsets int32 [B + 1]: the
+    rows of each sequence; seq_lens int32 [B]: its tokens with the new ones; block_table int32 [B, max_blocks]; cos, sin fp32
+    [positions, rot / 2] or None; Kc, Vc [num_blocks, H, block_size, D] of K's type."""
+    return _append("mlt_paged_append", Q, K, V, offsets, seq_lens, block_table, cos, sin, Kc, Vc, None, None, Qo, interleaved, stream)
+
+
+def mlt_paged_append_fp8(Q: torch.Tensor | None, K: torch.Tensor, V: torch.Tensor, offsets: torch.Tensor, seq_lens: torch.Tensor,
+                         block_table: torch.Tensor, cos: torch.Tensor | None, sin: torch.Tensor | None, Kc: torch.Tensor, Vc: torch.Tensor,
+                         Ks: torch.Tensor, Vs: torch.Tensor, Qo: torch.Tensor | None = None, interleaved: bool = False,
+                         stream=None) -> torch.Tensor | None:
+    """mlt_paged_append into an e4m3 cache with fp32 scales Ks, Vs [num_blocks, H], which are updated with it."""
+    if Ks is None or Vs is None:
+        raise ValueError("mlt_paged_append_fp8 needs the cache's scales")
+    return _append("mlt_paged_append_fp8", Q, K, V, offsets, seq_lens, block_table, cos, sin, Kc, Vc, Ks, Vs, Qo, interleaved, stream)
+
+
+def mlt_paged_attn_decode_fp8(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, Ks: torch.Tensor, Vs: torch.Tensor,
+                              block_table: torch.Tensor, seq_lens: torch.Tensor, scale: float, O: torch.Tensor | None = None,
+                              stream=None) -> torch.Tensor:
+    """Q [B, Hq, D]; Kc, Vc e4m3 [num_blocks, H, block_size, D] with Hq a multiple of H; Ks, Vs fp32 [num_blocks, H]; block_table
+    int32 [B, max_blocks]; seq_lens int32 [B], 0 for a sequence without keys (zeros); returns O [B, Hq, D]."""
+    name = "mlt_paged_attn_decode_fp8"
+    _gpu(name, Q, Kc, Vc, Ks, Vs, block_table, seq_lens, O)
+    dt = _dtype_code(Q)
+    if Q.dim() != 3 or Kc.dim() != 4 or Vc.shape != Kc.shape or Kc.shape[3] != Q.shape[2]:
+        raise ValueError("%s: cache shape does not match Q" % name)
+    if Kc.dtype != E4M3 or Vc.dtype != E4M3:
+        raise TypeError("%s: the cache must be of type float8_e4m3fn" % name)
+    B, Hq, D = Q.shape
+    nb, H, bs, _ = Kc.shape
+    for s in (Ks, Vs):
+        if s.dtype != torch.float32 or tuple(s.shape) != (nb, H):
+            raise ValueError("%s: Ks and Vs must be fp32 [num_blocks, H]" % name)
+    if block_table.dtype != torch.int32 or seq_lens.dtype != torch.int32:
+        raise ValueError("%s: block_table and seq_lens must be int32" % name)
+    if block_table.dim() != 2 or block_table.shape[0] != B or tuple(seq_lens.shape) != (B,):
+        raise ValueError("%s: block_table / seq_lens shape" % name)
+    if O is None:
+        O = torch.empty_like(Q, memory_format=torch.contiguous_format)
+    elif O.dtype != Q.dtype or O.shape != Q.shape:
+        raise ValueError("%s: O has the wrong dtype or shape" % name)
+    for t in (Q, Kc, Vc, Ks, Vs, block_table, seq_lens, O):
+        if not t.is_contiguous():
+            raise ValueError("%s: tensors must be contiguous" % name)
+    with _OtherDevice(Q.device):
+        rc = _lib.mlt_paged_attn_decode_fp8(B, Hq, H, D, bs, block_table.shape[1], nb, Q.data_ptr(), Kc.data_ptr(), Vc.data_ptr(), Ks.data_ptr(),
+                                            Vs.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), O.data_ptr(), float(scale), dt,
+                                            _stream(stream, Q.device))
+    if rc != MLT_OK:
+        raise MltError(rc, name)
     return O

@@ -142,6 +142,35 @@ struct TimedRegion {
   ~TimedRegion() { if (g_ev_stop) (void)hipEventRecord(g_ev_stop, s); }
 };
 
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+int append_call(const AppendArgs& a, bool fp8, void* stream) {
+  if (a.dtype != MLT_BF16 && a.dtype != MLT_FP16) return MLT_ERR_INVALID_ARG;
+  if (a.T < 0 || a.B < 0 || a.Hq < 0 || a.H < 0 || a.D <= 0 || a.block_size <= 0 || a.max_blocks <= 0 || a.num_blocks <= 0 || a.rot < 0 || a.rot > a.D)
+    return MLT_ERR_INVALID_ARG;
+  if (a.D != 64 && a.D != 128) return MLT_ERR_UNSUPPORTED;
+  if (a.block_size % 16 || a.block_size > 1024 || a.rot % 16) return MLT_ERR_UNSUPPORTED;
+  if (a.T == 0 || a.B == 0 || a.Hq + a.H == 0) return MLT_OK;
+  if (a.T > INT_MAX || a.B > INT_MAX / 4 || a.Hq > INT_MAX / 4 / a.D || a.H > INT_MAX / 4 / a.D || a.num_blocks > INT_MAX || a.max_blocks > INT_MAX ||
+      a.max_blocks * a.block_size > INT_MAX || a.positions > INT_MAX) return MLT_ERR_UNSUPPORTED;
+  if (!a.offsets || !a.seq_lens || !a.block_table || !aligned(a.offsets, 4) || !aligned(a.seq_lens, 4) || !aligned(a.block_table, 4)) return MLT_ERR_INVALID_ARG;
+  if (a.rot && (!a.cos || !a.sin || !aligned(a.cos, 4) || !aligned(a.sin, 4) || a.positions < 1)) return MLT_ERR_INVALID_ARG;
+  if (a.Hq && (!a.Q || !a.Qo || !aligned(a.Q, 16) || !aligned(a.Qo, 16) || a.ldq < a.Hq * a.D)) return MLT_ERR_INVALID_ARG;
+  if (a.H && (!a.K || !a.V || !a.Kc || !a.Vc || !aligned(a.K, 16) || !aligned(a.V, 16) || !aligned(a.Kc, 16) || !aligned(a.Vc, 16) || a.ldk < a.H * a.D ||
+              a.ldv < a.H * a.D)) return MLT_ERR_INVALID_ARG;
+  if (fp8 && a.H && (!a.Ks || !a.Vs || !aligned(a.Ks, 4) || !aligned(a.Vs, 4))) return MLT_ERR_INVALID_ARG;
+  if ((a.Hq && a.ldq % 8) || (a.H && (a.ldk % 8 || a.ldv % 8))) return MLT_ERR_UNSUPPORTED;
+  if (!device_is_gfx950()) return MLT_ERR_DEVICE;
+  hipStream_t s = (hipStream_t)stream;
+  int rc;
+  {
+    TimedRegion t(s);
+    rc = run_append(a, fp8, s);
+  }
+  if (rc == MLT_OK) g_last_kernel = fp8 ? "paged_append_fp8" : "paged_append";
+  return rc;
+}
+
 }  // namespace
 
 extern "C" {
@@ -316,6 +345,104 @@ int mlt_paged_attn_decode(int64_t B, int64_t H, int64_t D, int64_t block_size, i
     if (nsplit > 1) snprintf(name, sizeof name, "paged_decode_d%d_w4_keysplit%d", (int)D, nsplit);
     else snprintf(name, sizeof name, "paged_decode_d%d_w4", (int)D);
     g_last_kernel = name;
+  }
+  return rc;
+}
+
+int mlt_quant_fp8(int64_t M, int64_t K, const void* X, int64_t ldx, int64_t block_rows, void* Xq, int64_t ldq, float* S,
+                  int64_t lds, int dtype, void* stream) {
+  if (dtype != MLT_BF16 && dtype != MLT_FP16) return MLT_ERR_INVALID_ARG;
+  if (M < 0 || K < 0 || block_rows <= 0) return MLT_ERR_INVALID_ARG;
+  if (block_rows != 1 && block_rows != 128) return MLT_ERR_UNSUPPORTED;
+  if (M == 0 || K == 0) return MLT_OK;
+  if (M > INT_MAX - 128 || K > INT_MAX - 512) return MLT_ERR_UNSUPPORTED;
+  if (!X || !Xq || !S || ldx < K || ldq < K || lds < (M + block_rows - 1) / block_rows) return MLT_ERR_INVALID_ARG;
+  if (!aligned(X, 16) || !aligned(Xq, 16) || !aligned(S, 4)) return MLT_ERR_INVALID_ARG;
+  if (K % 8 || (M > 1 && (ldx % 8 || ldq % 16))) return MLT_ERR_UNSUPPORTED;
+  if (!device_is_gfx950()) return MLT_ERR_DEVICE;
+  QuantArgs a{M, K, (const uint16_t*)X, ldx, block_rows, (uint8_t*)Xq, ldq, S, lds, dtype};
+  hipStream_t s = (hipStream_t)stream;
+  int rc;
+  {
+    TimedRegion t(s);
+    rc = run_quant(a, s);
+  }
+  if (rc == MLT_OK) g_last_kernel = block_rows == 1 ? "quant_fp8_rows" : "quant_fp8_tiles";
+  return rc;
+}
+
+int mlt_gemm_fp8(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const float* Sa, int64_t ldsa, const void* B,
+                 int64_t ldb, const float* Sb, int64_t ldsb, void* C, int64_t ldc, int dtype, void* stream) {
+  if (dtype != MLT_BF16 && dtype != MLT_FP16) return MLT_ERR_INVALID_ARG;
+  if (M < 0 || N < 0 || K < 0) return MLT_ERR_INVALID_ARG;
+  if (M == 0 || N == 0) return MLT_OK;
+  if (M > INT_MAX - 256 || N > INT_MAX - 256 || K > INT_MAX - 256) return MLT_ERR_UNSUPPORTED;
+  if (!C || ldc < N || !aligned(C, 2)) return MLT_ERR_INVALID_ARG;
+  if (K > 0) {
+    if (!A || !B || !Sa || !Sb || lda < K || ldb < K || ldsa < M || ldsb < (N + 127) / 128) return MLT_ERR_INVALID_ARG;
+    if (!aligned(A, 16) || !aligned(B, 16) || !aligned(Sa, 4) || !aligned(Sb, 4)) return MLT_ERR_INVALID_ARG;
+    if (K % 16 || lda % 16 || ldb % 16) return MLT_ERR_UNSUPPORTED;
+    if (256 * (lda > ldb ? lda : ldb) >= ((int64_t)1 << 31)) return MLT_ERR_UNSUPPORTED;   // 32-bit offsets inside a tile
+  }
+  if (!device_is_gfx950()) return MLT_ERR_DEVICE;
+  GemmFp8Args a{M, N, K, (const uint8_t*)A, lda, Sa, ldsa, (const uint8_t*)B, ldb, Sb, ldsb, (uint16_t*)C, ldc, dtype};
+  hipStream_t s = (hipStream_t)stream;
+  const char* name = "";
+  int rc;
+  {
+    TimedRegion t(s);
+    rc = run_gemm_fp8(a, s, &name);
+  }
+  if (rc == MLT_OK) g_last_kernel = name;
+  return rc;
+}
+
+int mlt_paged_append(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks,
+                     int64_t num_blocks, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                     const int32_t* offsets, const int32_t* seq_lens, const int32_t* block_table, const float* cos, const float* sin,
+                     int64_t rot, int64_t positions, int interleaved, void* Qo, void* Kc, void* Vc, int dtype, void* stream) {
+  AppendArgs a{T, B, Hq, H, D, block_size, max_blocks, num_blocks, (const uint16_t*)Q, ldq, (const uint16_t*)K, ldk, (const uint16_t*)V, ldv,
+               offsets, seq_lens, block_table, cos, sin, rot, positions, interleaved ? 1 : 0, (uint16_t*)Qo, Kc, Vc, nullptr, nullptr, dtype};
+  return append_call(a, false, stream);
+}
+
+int mlt_paged_append_fp8(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks,
+                         int64_t num_blocks, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V, int64_t ldv,
+                         const int32_t* offsets, const int32_t* seq_lens, const int32_t* block_table, const float* cos,
+                         const float* sin, int64_t rot, int64_t positions, int interleaved, void* Qo, void* Kc, void* Vc, float* Ks,
+                         float* Vs, int dtype, void* stream) {
+  AppendArgs a{T, B, Hq, H, D, block_size, max_blocks, num_blocks, (const uint16_t*)Q, ldq, (const uint16_t*)K, ldk, (const uint16_t*)V, ldv,
+               offsets, seq_lens, block_table, cos, sin, rot, positions, interleaved ? 1 : 0, (uint16_t*)Qo, Kc, Vc, Ks, Vs, dtype};
+  return append_call(a, true, stream);
+}
+
+int mlt_paged_attn_decode_fp8(int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks,
+                              int64_t num_blocks, const void* Q, const void* Kc, const void* Vc, const float* Ks, const float* Vs,
+                              const int32_t* block_table, const int32_t* seq_lens, void* O, float scale, int dtype, void* stream) {
+  if (dtype != MLT_BF16 && dtype != MLT_FP16) return MLT_ERR_INVALID_ARG;
+  if (B < 0 || Hq < 0 || H < 0 || D <= 0 || block_size <= 0 || max_blocks <= 0 || num_blocks <= 0) return MLT_ERR_INVALID_ARG;
+  if (!(scale == scale) || scale - scale != 0.f) return MLT_ERR_INVALID_ARG;   // NaN or infinite
+  if (D != 64 && D != 128) return MLT_ERR_UNSUPPORTED;
+  if (block_size % 16 || block_size > 1024) return MLT_ERR_UNSUPPORTED;
+  if (B == 0 || Hq == 0) return MLT_OK;
+  if (H == 0 || Hq % H) return MLT_ERR_INVALID_ARG;
+  if (!Q || !Kc || !Vc || !Ks || !Vs || !block_table || !seq_lens || !O) return MLT_ERR_INVALID_ARG;
+  if (!aligned(Q, 16) || !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(O, 2) || !aligned(Ks, 4) || !aligned(Vs, 4) || !aligned(block_table, 4) ||
+      !aligned(seq_lens, 4)) return MLT_ERR_INVALID_ARG;
+  if (B > INT_MAX || Hq > INT_MAX || B * Hq > INT_MAX || max_blocks > INT_MAX || max_blocks * block_size > INT_MAX || num_blocks > INT_MAX) return MLT_ERR_UNSUPPORTED;
+  if (!device_is_gfx950()) return MLT_ERR_DEVICE;
+  PagedFp8Args a{B, Hq, H, D, block_size, max_blocks, num_blocks, (const uint16_t*)Q, (const uint8_t*)Kc, (const uint8_t*)Vc, Ks, Vs, block_table,
+                 seq_lens, (uint16_t*)O, scale, dtype, overrides().key_split};
+  hipStream_t s = (hipStream_t)stream;
+  int rc, nsplit = 1;
+  {
+    TimedRegion t(s);
+    rc = run_paged_fp8(a, s, &nsplit);
+  }
+  if (rc == MLT_OK) {
+    if (nsplit > 1) snprintf(g_name_buf, sizeof g_name_buf, "paged_decode_fp8_d%d_w4_keysplit%d", (int)D, nsplit);
+    else snprintf(g_name_buf, sizeof g_name_buf, "paged_decode_fp8_d%d_w4", (int)D);
+    g_last_kernel = g_name_buf;
   }
   return rc;
 }

@@ -181,6 +181,54 @@ int run_paged_decode(const PagedArgs& a, hipStream_t s, int* nsplit_out);
 int plan_paged_split(const PagedArgs& a);                                       // key ranges per (sequence, head)
 bool paged_by_length(const PagedArgs& a, int64_t nsplit, int64_t ncu);   // workgroups dealt out by sequence length?
 
+// The 8-bit operators (arguments as in include/mlt.h)
+struct QuantArgs {
+  int64_t M, K;
+  const uint16_t* X; int64_t ldx;
+  int64_t block_rows;
+  uint8_t* Xq; int64_t ldq;
+  float* S; int64_t lds;
+  int dtype;
+};
+int run_quant(const QuantArgs& a, hipStream_t s);   // quant.hip
+struct GemmFp8Args {
+  int64_t M, N, K;
+  const uint8_t* A; int64_t lda;
+  const float* Sa; int64_t ldsa;
+  const uint8_t* B; int64_t ldb;
+  const float* Sb; int64_t ldsb;
+  uint16_t* C; int64_t ldc;
+  int dtype;
+};
+int run_gemm_fp8(const GemmFp8Args& a, hipStream_t s, const char** name);   // gemm_fp8.hip
+struct AppendArgs {
+  int64_t T, B, Hq, H, D, block_size, max_blocks, num_blocks;
+  const uint16_t* Q; int64_t ldq;
+  const uint16_t* K; int64_t ldk;
+  const uint16_t* V; int64_t ldv;
+  const int32_t *offsets, *seq_lens, *block_table;
+  const float *cos, *sin;
+  int64_t rot, positions;
+  int interleaved;
+  uint16_t* Qo;
+  void *Kc, *Vc;
+  float *Ks, *Vs;            // an 8-bit cache's
+  int dtype;
+};
+int run_append(const AppendArgs& a, bool fp8, hipStream_t s);   // append.hip
+struct PagedFp8Args {
+  int64_t B, Hq, H, D, block_size, max_blocks, num_blocks;
+  const uint16_t* Q;
+  const uint8_t *Kc, *Vc;
+  const float *Ks, *Vs;
+  const int32_t *block_table, *seq_lens;
+  uint16_t* O;
+  float scale;
+  int dtype;
+  int forced_split = 0;      // as in PagedArgs
+};
+int run_paged_fp8(const PagedFp8Args& a, hipStream_t s, int* nsplit_out);   // paged_fp8.hip
+
 // The library's own scratch memory for a stream of the current device: at least `bytes`, behind its counters, kept
 // (and grown by doubling) from call to call, never freed; nullptr if it cannot be had, and while the
 // stream records into a graph. Work of one stream that uses it is ordered by the stream.
