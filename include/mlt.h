@@ -199,7 +199,8 @@ int mlt_quant_fp8(int64_t M, int64_t K, const void* X, int64_t ldx, int64_t bloc
 /*
  * The matrix product of e4m3 operands with block scales, C = A * B^T with B stored N x K:
  *   C[m][n] = sum over kb of Sa[kb][m] * Sb[kb][n / 128] * sum over k = 128 kb .. 128 kb + 127 of A[m][k] * B[n][k]
- * The sum over a block and the sum over the blocks are fp32; C is rounded once to `dtype`.
+ * The sum over a block and the sum over the blocks are fp32; C is rounded once to `dtype`. The order of the sums goes by the
+ * sizes and by B's alignment; equal calls give equal bits.
  *   A       device, M x K row-major e4m3, row stride lda >= K
  *   Sa      device, fp32 [ceil(K / 128)][M], row stride ldsa >= M
  *   B       device, N x K row-major e4m3, row stride ldb >= K

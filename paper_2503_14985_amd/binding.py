@@ -100,7 +100,7 @@ class MltError(RuntimeError):
 # It is built against one torch, whose tensors it looks into; with another one, with a torch without ROCm, or where it has not been built,
 # every call goes through the functions below.
 class _PythonOnly:
-    gemm = gemm_acc = gemm_bias_act = mha_fwd = paged_attn_decode = staticmethod(lambda *args: None)
+    gemm = gemm_acc = gemm_bias_act = mha_fwd = paged_attn_decode = quant_fp8 = gemm_fp8 = paged_append = paged_attn_decode_fp8 = staticmethod(lambda *args: None)
 
 
 _fast = _PythonOnly
@@ -108,7 +108,8 @@ try:
     from . import _fastcall
     if _fastcall.torch_version == torch.__version__:
         _fastcall.bind(MltError, *(ctypes.cast(getattr(_lib, _f), _p).value for _f in (
-            "mlt_gemm", "mlt_gemm_bias_act", "mlt_gemm_acc", "mlt_mha_fwd", "mlt_paged_attn_decode")))
+            "mlt_gemm", "mlt_gemm_bias_act", "mlt_gemm_acc", "mlt_mha_fwd", "mlt_paged_attn_decode", "mlt_quant_fp8", "mlt_gemm_fp8", "mlt_paged_append",
+            "mlt_paged_append_fp8", "mlt_paged_attn_decode_fp8")))
         _fast = _fastcall
 except ImportError:
     pass
@@ -444,6 +445,9 @@ def _scales(t: torch.Tensor, shape, name: str) -> int:
 def mlt_quant_fp8(X: torch.Tensor, block_rows: int = 1, Xq: torch.Tensor | None = None, S: torch.Tensor | None = None, stream=None):
     """Xq (e4m3 [M, K]) and S (fp32 [ceil(K/128), ceil(M/block_rows)]) of X [M, K]: a power of two as the scale of every
     block_rows x 128 block. block_rows: 1 (activations) or 128 (weights)."""
+    done = _fast.quant_fp8(X, block_rows, Xq, S, stream)
+    if done is not None:
+        return done
     _gpu("mlt_quant_fp8", X, Xq, S)
     dt, ldx = _dtype_code(X), _rows_contiguous(X, "X")
     M, K = X.shape
@@ -467,6 +471,9 @@ def mlt_gemm_fp8(A: torch.Tensor, Sa: torch.Tensor, B: torch.Tensor, Sb: torch.T
                  dtype: torch.dtype = torch.bfloat16, stream=None) -> torch.Tensor:
     """C = (A * Sa) @ (B * Sb).T: A [M, K], B [N, K] e4m3, Sa [ceil(K/128), M] and Sb [ceil(K/128), ceil(N/128)] fp32, as
     mlt_quant_fp8 makes them with block_rows 1 and 128. C (`dtype`, where it is not given) is bf16 or fp16 [M, N]."""
+    done = _fast.gemm_fp8(A, Sa, B, Sb, C, stream)
+    if done is not None:
+        return done
     _gpu("mlt_gemm_fp8", A, Sa, B, Sb, C)
     if A.dtype != E4M3 or B.dtype != E4M3:
         raise TypeError("A and B must be float8_e4m3fn tensors")
@@ -500,6 +507,9 @@ def _head_rows(t: torch.Tensor, T: int, D: int, dtype, name: str) -> int:
 
 
 def _append(name: str, Q, K, V, offsets, seq_lens, block_table, cos, sin, Kc, Vc, Ks, Vs, Qo, interleaved, stream):
+    done = _fast.paged_append(Q, K, V, offsets, seq_lens, block_table, cos, sin, Kc, Vc, Ks, Vs, Qo, interleaved, stream)
+    if done is not None:
+        return done
     _gpu(name, K, V, Q, offsets, seq_lens, block_table, cos, sin, Kc, Vc, Ks, Vs, Qo)
     dt = _dtype_code(K)
     if K.dim() != 3:
@@ -579,6 +589,9 @@ def mlt_paged_attn_decode_fp8(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tenso
     """Q [B, Hq, D]; Kc, Vc e4m3 [num_blocks, H, block_size, D] with Hq a multiple of H; Ks, Vs fp32 [num_blocks, H]; block_table
     int32 [B, max_blocks]; seq_lens int32 [B], 0 for a sequence without keys (zeros); returns O [B, Hq, D]."""
     name = "mlt_paged_attn_decode_fp8"
+    done = _fast.paged_attn_decode_fp8(Q, Kc, Vc, Ks, Vs, block_table, seq_lens, scale, O, stream)
+    if done is not None:
+        return done
     _gpu(name, Q, Kc, Vc, Ks, Vs, block_table, seq_lens, O)
     dt = _dtype_code(Q)
     if Q.dim() != 3 or Kc.dim() != 4 or Vc.shape != Kc.shape or Kc.shape[3] != Q.shape[2]:

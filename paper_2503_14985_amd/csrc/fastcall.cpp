@@ -22,6 +22,11 @@ decltype(&mlt_gemm_bias_act) call_gemm_bias_act;
 decltype(&mlt_gemm_acc) call_gemm_acc;
 decltype(&mlt_mha_fwd) call_mha_fwd;
 decltype(&mlt_paged_attn_decode) call_paged;
+decltype(&mlt_quant_fp8) call_quant_fp8;
+decltype(&mlt_gemm_fp8) call_gemm_fp8;
+decltype(&mlt_paged_append) call_append;
+decltype(&mlt_paged_append_fp8) call_append_fp8;
+decltype(&mlt_paged_attn_decode_fp8) call_paged_fp8;
 PyObject* error_class;      // binding.MltError(status, where)
 
 // A plain tensor with memory of its own kind on GPU `device` (-1: the first one sets it), or null
@@ -188,6 +193,148 @@ PyObject* py_paged(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return result(rc, v[6], "mlt_paged_attn_decode");
 }
 
+// ---- the 8-bit operators
+
+bool is(const at::Tensor& t, at::ScalarType type) { return t.scalar_type() == type; }
+bool sized(const at::Tensor& t, int64_t a, int64_t b) { return t.dim() == 2 && t.size(0) == a && t.size(1) == b; }
+
+// quant_fp8(X, block_rows, Xq, S, stream)
+PyObject* py_quant_fp8(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 5 || v[4] != Py_None || !PyLong_CheckExact(v[1])) Py_RETURN_NONE;
+  int overflow = 0, device = -1;
+  const long rows = PyLong_AsLongAndOverflow(v[1], &overflow);
+  if (overflow || rows < 1) Py_RETURN_NONE;
+  const at::Tensor *x = plain(v[0], device), *q = x ? plain(v[2], device) : nullptr, *s = q ? plain(v[3], device) : nullptr;
+  if (!s) Py_RETURN_NONE;
+  const int dtype = dtype_code(*x);
+  const int64_t ldx = row_stride(*x), ldq = row_stride(*q), lds = row_stride(*s);
+  if (dtype < 0 || ldx < 0 || ldq < 0 || lds < 0 || !is(*q, at::kFloat8_e4m3fn) || !is(*s, at::kFloat) || q->sizes() != x->sizes()) Py_RETURN_NONE;
+  const int64_t M = x->size(0), K = x->size(1);
+  if (!sized(*s, (K + 127) / 128, (M + rows - 1) / rows)) Py_RETURN_NONE;
+  void* stream;
+  if (!on_current_device(device, &stream)) Py_RETURN_NONE;
+  void *px = x->data_ptr(), *pq = q->data_ptr(), *ps = s->data_ptr();
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = call_quant_fp8(M, K, px, ldx, rows, pq, ldq, (float*)ps, lds, dtype, stream);
+  Py_END_ALLOW_THREADS
+  PyObject* out = PyTuple_Pack(2, v[2], v[3]);
+  if (!out) return nullptr;
+  PyObject* r = result(rc, out, "mlt_quant_fp8");
+  Py_DECREF(out);
+  return r;
+}
+
+// gemm_fp8(A, Sa, B, Sb, C, stream)
+PyObject* py_gemm_fp8(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 6 || v[5] != Py_None) Py_RETURN_NONE;
+  int device = -1;
+  const at::Tensor* t[5];
+  int64_t ld[5];
+  for (int i = 0; i < 5; ++i) {
+    t[i] = plain(v[i], device);
+    if (!t[i] || (ld[i] = row_stride(*t[i])) < 0) Py_RETURN_NONE;
+  }
+  const at::Tensor &a = *t[0], &sa = *t[1], &b = *t[2], &sb = *t[3], &c = *t[4];
+  const int dtype = dtype_code(c);
+  if (dtype < 0 || !is(a, at::kFloat8_e4m3fn) || !is(b, at::kFloat8_e4m3fn) || !is(sa, at::kFloat) || !is(sb, at::kFloat)) Py_RETURN_NONE;
+  const int64_t M = a.size(0), K = a.size(1), N = b.size(0), kb = (K + 127) / 128;
+  if (b.size(1) != K || !sized(sa, kb, M) || !sized(sb, kb, (N + 127) / 128) || !sized(c, M, N)) Py_RETURN_NONE;
+  void* stream;
+  if (!on_current_device(device, &stream)) Py_RETURN_NONE;
+  void* p[5];
+  for (int i = 0; i < 5; ++i) p[i] = t[i]->data_ptr();
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = call_gemm_fp8(M, N, K, p[0], ld[0], (const float*)p[1], ld[1], p[2], ld[2], (const float*)p[3], ld[3], p[4], ld[4], dtype, stream);
+  Py_END_ALLOW_THREADS
+  return result(rc, v[4], "mlt_gemm_fp8");
+}
+
+// Row stride of [T, heads, D] whose heads lie side by side, or -1
+int64_t head_rows(const at::Tensor& t, int64_t T, int64_t D) {
+  if (t.dim() != 3 || t.size(0) != T || t.size(2) != D || (D > 1 && t.stride(2) != 1) || (t.size(1) > 1 && t.stride(1) != D)) return -1;
+  return T > 1 ? t.stride(0) : t.size(1) * D;
+}
+
+// paged_append(Q, K, V, offsets, seq_lens, block_table, cos, sin, Kc, Vc, Ks, Vs, Qo, interleaved, stream): with queries, angles and a
+// Qo; without Ks and Vs (None): the 16-bit cache
+PyObject* py_append(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 15 || v[14] != Py_None || !PyBool_Check(v[13])) Py_RETURN_NONE;
+  const bool fp8 = v[10] != Py_None;
+  int device = -1;
+  const at::Tensor* t[13];
+  for (int i = 0; i < 13; ++i) {
+    t[i] = nullptr;
+    if (!fp8 && (i == 10 || i == 11)) continue;
+    t[i] = plain(v[i], device);
+    if (!t[i] || (i > 2 && !t[i]->is_contiguous())) Py_RETURN_NONE;
+  }
+  const at::Tensor &q = *t[0], &k = *t[1], &vv = *t[2], &offsets = *t[3], &lens = *t[4], &table = *t[5], &cs = *t[6], &sn = *t[7], &kc = *t[8], &vc = *t[9], &qo = *t[12];
+  const int dtype = dtype_code(k);
+  if (dtype < 0 || k.dim() != 3 || q.dim() != 3 || !is(q, k.scalar_type()) || !is(vv, k.scalar_type()) || !is(qo, k.scalar_type())) Py_RETURN_NONE;
+  const int64_t T = k.size(0), H = k.size(1), D = k.size(2), Hq = q.size(1);
+  const int64_t ldq = head_rows(q, T, D), ldk = head_rows(k, T, D), ldv = head_rows(vv, T, D);
+  if (ldq < 0 || ldk < 0 || ldv < 0 || vv.size(1) != H || qo.sizes() != q.sizes()) Py_RETURN_NONE;
+  if (!is(offsets, at::kInt) || !is(lens, at::kInt) || !is(table, at::kInt) || offsets.dim() != 1 || lens.dim() != 1 || table.dim() != 2) Py_RETURN_NONE;
+  const int64_t B = lens.size(0);
+  if (offsets.size(0) != B + 1 || table.size(0) != B) Py_RETURN_NONE;
+  if (!is(cs, at::kFloat) || !is(sn, at::kFloat) || cs.dim() != 2 || cs.sizes() != sn.sizes()) Py_RETURN_NONE;
+  const at::ScalarType want = fp8 ? at::kFloat8_e4m3fn : k.scalar_type();
+  if (!is(kc, want) || !is(vc, want) || kc.dim() != 4 || kc.size(1) != H || kc.size(3) != D || vc.sizes() != kc.sizes()) Py_RETURN_NONE;
+  const int64_t nb = kc.size(0);
+  for (int i = 10; fp8 && i < 12; ++i)
+    if (!is(*t[i], at::kFloat) || !sized(*t[i], nb, H)) Py_RETURN_NONE;
+  void* stream;
+  if (!on_current_device(device, &stream)) Py_RETURN_NONE;
+  void* p[13];
+  for (int i = 0; i < 13; ++i) p[i] = t[i] ? t[i]->data_ptr() : nullptr;
+  const int64_t bs = kc.size(2), per = table.size(1), rot = 2 * cs.size(1), positions = cs.size(0);
+  const int pairs = v[13] == Py_True;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  if (fp8)
+    rc = call_append_fp8(T, B, Hq, H, D, bs, per, nb, p[0], ldq, p[1], ldk, p[2], ldv, (const int32_t*)p[3], (const int32_t*)p[4], (const int32_t*)p[5], (const float*)p[6],
+                         (const float*)p[7], rot, positions, pairs, p[12], p[8], p[9], (float*)p[10], (float*)p[11], dtype, stream);
+  else
+    rc = call_append(T, B, Hq, H, D, bs, per, nb, p[0], ldq, p[1], ldk, p[2], ldv, (const int32_t*)p[3], (const int32_t*)p[4], (const int32_t*)p[5], (const float*)p[6],
+                     (const float*)p[7], rot, positions, pairs, p[12], p[8], p[9], dtype, stream);
+  Py_END_ALLOW_THREADS
+  return result(rc, v[12], fp8 ? "mlt_paged_append_fp8" : "mlt_paged_append");
+}
+
+// paged_attn_decode_fp8(Q, Kc, Vc, Ks, Vs, block_table, seq_lens, scale, O, stream)
+PyObject* py_paged_fp8(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 10 || v[9] != Py_None || !PyFloat_CheckExact(v[7])) Py_RETURN_NONE;
+  int device = -1;
+  const at::Tensor* t[8];
+  PyObject* const o[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[8]};
+  for (int i = 0; i < 8; ++i) {
+    t[i] = plain(o[i], device);
+    if (!t[i] || !t[i]->is_contiguous()) Py_RETURN_NONE;
+  }
+  const at::Tensor &q = *t[0], &kc = *t[1], &vc = *t[2], &table = *t[5], &lens = *t[6], &out = *t[7];
+  const int dtype = dtype_code(q);
+  if (dtype < 0 || q.dim() != 3 || kc.dim() != 4 || kc.size(3) != q.size(2) || vc.sizes() != kc.sizes()) Py_RETURN_NONE;
+  if (!is(kc, at::kFloat8_e4m3fn) || !is(vc, at::kFloat8_e4m3fn)) Py_RETURN_NONE;
+  const int64_t nb = kc.size(0), H = kc.size(1), B = q.size(0);
+  for (int i = 3; i < 5; ++i)
+    if (!is(*t[i], at::kFloat) || !sized(*t[i], nb, H)) Py_RETURN_NONE;
+  if (!is(table, at::kInt) || !is(lens, at::kInt) || table.dim() != 2 || lens.dim() != 1 || table.size(0) != B || lens.size(0) != B) Py_RETURN_NONE;
+  if (!is(out, q.scalar_type()) || out.sizes() != q.sizes()) Py_RETURN_NONE;
+  void* stream;
+  if (!on_current_device(device, &stream)) Py_RETURN_NONE;
+  void* p[8];
+  for (int i = 0; i < 8; ++i) p[i] = t[i]->data_ptr();
+  const int64_t Hq = q.size(1), D = q.size(2), bs = kc.size(2), per = table.size(1);
+  const float scale = (float)PyFloat_AS_DOUBLE(v[7]);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = call_paged_fp8(B, Hq, H, D, bs, per, nb, p[0], p[1], p[2], (const float*)p[3], (const float*)p[4], (const int32_t*)p[5], (const int32_t*)p[6], p[7], scale, dtype, stream);
+  Py_END_ALLOW_THREADS
+  return result(rc, v[8], "mlt_paged_attn_decode_fp8");
+}
+
 // A torch error in here (a tensor without memory behind it, say) is binding.py's to meet again
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* v, Py_ssize_t n) {
@@ -199,11 +346,12 @@ PyObject* guarded(PyObject* self, PyObject* const* v, Py_ssize_t n) {
   }
 }
 
-// bind(error class, gemm, gemm_bias_act, gemm_acc, mha_fwd, paged_attn_decode): the library functions' addresses
+// bind(error class, gemm, gemm_bias_act, gemm_acc, mha_fwd, paged_attn_decode[, quant_fp8, gemm_fp8, paged_append, paged_append_fp8,
+// paged_attn_decode_fp8]): the library functions' addresses; those that are left out stay as they are
 PyObject* py_bind(PyObject*, PyObject* args) {
-  Py_ssize_t a[5];
+  Py_ssize_t a[10] = {};
   PyObject* err;
-  if (!PyArg_ParseTuple(args, "Onnnnn", &err, &a[0], &a[1], &a[2], &a[3], &a[4])) return nullptr;
+  if (!PyArg_ParseTuple(args, "Onnnnn|nnnnn", &err, &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &a[9])) return nullptr;
   Py_INCREF(err);
   error_class = err;
   call_gemm = reinterpret_cast<decltype(call_gemm)>(a[0]);
@@ -211,6 +359,11 @@ PyObject* py_bind(PyObject*, PyObject* args) {
   call_gemm_acc = reinterpret_cast<decltype(call_gemm_acc)>(a[2]);
   call_mha_fwd = reinterpret_cast<decltype(call_mha_fwd)>(a[3]);
   call_paged = reinterpret_cast<decltype(call_paged)>(a[4]);
+  if (a[5]) call_quant_fp8 = reinterpret_cast<decltype(call_quant_fp8)>(a[5]);
+  if (a[6]) call_gemm_fp8 = reinterpret_cast<decltype(call_gemm_fp8)>(a[6]);
+  if (a[7]) call_append = reinterpret_cast<decltype(call_append)>(a[7]);
+  if (a[8]) call_append_fp8 = reinterpret_cast<decltype(call_append_fp8)>(a[8]);
+  if (a[9]) call_paged_fp8 = reinterpret_cast<decltype(call_paged_fp8)>(a[9]);
   Py_RETURN_NONE;
 }
 
@@ -220,6 +373,10 @@ PyMethodDef methods[] = {MLT_FAST("gemm", py_gemm),
                          MLT_FAST("gemm_bias_act", py_gemm_bias_act),
                          MLT_FAST("mha_fwd", py_mha_fwd),
                          MLT_FAST("paged_attn_decode", py_paged),
+                         MLT_FAST("quant_fp8", py_quant_fp8),
+                         MLT_FAST("gemm_fp8", py_gemm_fp8),
+                         MLT_FAST("paged_append", py_append),
+                         MLT_FAST("paged_attn_decode_fp8", py_paged_fp8),
                          {"bind", py_bind, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -266,6 +266,17 @@ int run_fp8_t(const GemmFp8Args& a, hipStream_t s, const char** name) {
   }
   DeviceInfo di;
   const int64_t ncu = device_info(di) && di.ncu > 0 ? di.ncu : 256;
+  if (a.M <= 64) {
+    int parts = a.forced_parts > 1 ? a.forced_parts : 1;
+    float* part = nullptr;
+    if (parts > 1) {
+      part = cached_scratch(parts * a.M * a.N * (int64_t)sizeof(float), s);
+      if (!part) parts = 1;
+    }
+    static const char* const names[9] = {"", "gemm_fp8_skinny", "gemm_fp8_skinny_splitk2", "", "gemm_fp8_skinny_splitk4", "", "", "", "gemm_fp8_skinny_splitk8"};
+    *name = names[parts];
+    return run_gemm_fp8_skinny(a, parts, part, s);
+  }
   const int64_t big = ((a.M + 255) / 256) * ((a.N + 255) / 256);
   if (big >= ncu) {
     *name = "gemm_fp8_256x256";

@@ -199,7 +199,9 @@ struct GemmFp8Args {
   const float* Sb; int64_t ldsb;
   uint16_t* C; int64_t ldc;
   int dtype;
+  int forced_parts = 0;      // as in GemmArgs
 };
+int run_gemm_fp8_skinny(const GemmFp8Args& a, int parts, float* part, hipStream_t s);   // gemm_fp8_skinny.hip: M <= 64; part: parts * M * N floats behind their counters
 int run_gemm_fp8(const GemmFp8Args& a, hipStream_t s, const char** name);   // gemm_fp8.hip
 struct AppendArgs {
   int64_t T, B, Hq, H, D, block_size, max_blocks, num_blocks;

@@ -129,7 +129,27 @@ def test_gemm(lib, dtype, M, N, K):
     rest[:M, 2:2 + N] = -7.0
     assert bool((rest == -7.0).all())
     again = lib.mlt_gemm_fp8(a.to(dev()), sa.to(dev()), b.to(dev()), sb.to(dev()), dtype=dtype)
-    assert torch.equal(again.view(torch.int16), out.contiguous().view(torch.int16))          # strides do not change a bit
+    gemm_check(again, a, sa, b, sb, dtype, K)                # (equal up to the order of the sums, which goes by B's alignment, too)
+
+
+@pytest.fixture
+def k_parts(lib):
+    yield lib.mlt_diag_force_k_parts
+    lib.mlt_diag_force_k_parts(0)
+
+
+@pytest.mark.parametrize("parts", [2, 4, 8])
+@pytest.mark.parametrize("M,N,K", [(1, 64, 128), (3, 1030, 2048), (16, 4096, 4112), (30, 520, 1040), (64, 2000, 2304), (50, 5000, 1024)])
+def test_gemm_k_split_across_workgroups(lib, k_parts, parts, M, N, K):
+    """Parts of K by workgroups of their own, some of them empty, added by the last one; the same bits on every run."""
+    k_parts(parts)
+    a, sa, b, sb = gemm_operands(M, N, K, M + N + K + parts)
+    at = [t.to(dev()) for t in (a, sa, b, sb)]
+    C = lib.mlt_gemm_fp8(*at)
+    assert lib.mlt_last_kernel().endswith("_splitk%d" % parts)
+    gemm_check(C, a, sa, b, sb, BF16, K)
+    for _ in range(4):
+        assert torch.equal(lib.mlt_gemm_fp8(*at).view(torch.int16), C.view(torch.int16))
 
 
 def test_gemm_large_sampled(lib):
@@ -594,3 +614,93 @@ def test_caches_past_4_gib(lib):
             assert (np.abs(vv - f64(v)[t0:t1, h]) <= u.HALF[F8] * np.abs(f64(v)[t0:t1, h]) + 2.0 ** -6 * 2.0 ** -10).all()
             o, mass, reach = u.attn(f64(q)[b, h], kk, vv, 0.1)
             assert (np.abs(f64(O)[b, h] - o) <= u.attn_tolerance(o, mass, reach, t1 - t0, D, BF16, np.abs(vv).max())).all()
+
+
+# ---- the binding's native call path
+
+def test_native_and_python_paths_agree(lib, monkeypatch):
+    """What the native path takes gives the bits of the step-by-step path; what it does not take (an output to allocate, a stream, a missing Q,
+    another type) it leaves to that."""
+    w, st = layer_setup(lib, 3, 109)
+    x = rand((3, 384), BF16, 113).to(dev())
+    f8 = lambda *s: torch.zeros(s, device=dev()).to(F8)  # noqa: E731
+    q, s = f8(3, 384), torch.empty((3, 3), device=dev())
+    lib.mlt_quant_fp8(x, Xq=q, S=s)
+    rows = rand((3, 8, 64), BF16, 127).to(dev())
+    st["where"][1] += 1
+    wide = torch.empty((3, 400), dtype=BF16, device=dev())
+    calls = {"quant_fp8": lambda: lib.mlt_quant_fp8(x, 1, Xq=f8(3, 384), S=torch.empty((3, 3), device=dev())),
+             "gemm_fp8": lambda: lib.mlt_gemm_fp8(q, s, *w["in"], C=torch.empty((3, 512), dtype=FP16, device=dev())),
+             "paged_append": lambda: lib.mlt_paged_append_fp8(rows[:, :4], rows[:, 4:6], rows[:, 6:], *st["where"], st["cos"], st["sin"], st["Kc"], st["Vc"], st["Ks"], st["Vs"],
+                                                              Qo=torch.empty((3, 4, 64), dtype=BF16, device=dev())),
+             "paged_attn_decode_fp8": lambda: lib.mlt_paged_attn_decode_fp8(rows[:, :4].contiguous(), st["Kc"], st["Vc"], st["Ks"], st["Vs"], st["where"][2], st["where"][1], 0.1,
+                                                                            O=torch.empty((3, 4, 64), dtype=BF16, device=dev()))}
+    sixteen = lambda: lib.mlt_paged_append(rows[:, :4], rows[:, 4:6], rows[:, 6:], *st["where"], st["cos"], st["sin"], torch.zeros((18, 2, 16, 64), dtype=BF16, device=dev()),  # noqa: E731
+                                           torch.zeros((18, 2, 16, 64), dtype=BF16, device=dev()), Qo=torch.empty((3, 4, 64), dtype=BF16, device=dev()))
+    taken = []
+    native = {f: getattr(lib._fast, f) for f in calls}
+
+    class Fast:
+        def __getattr__(self, f):
+            def call(*a):
+                r = native[f](*a)
+                taken.append(r is not None)
+                return r
+            return call
+
+    class Off:
+        def __getattr__(self, f):
+            return lambda *a: None
+
+    todo = list(calls.values()) + [sixteen]
+    monkeypatch.setattr(lib, "_fast", Fast())
+    got = [c() for c in todo]
+    assert taken == [True] * len(todo)
+    monkeypatch.setattr(lib, "_fast", Off())
+    bits = lambda t: [i.contiguous().view(torch.uint8).clone() for i in (t if isinstance(t, tuple) else (t,))]  # noqa: E731
+    for c, g in zip(todo, got):
+        assert all(torch.equal(i, j) for i, j in zip(bits(c()), bits(g)))
+    side = torch.cuda.Stream()
+    z = st["where"]
+    for f, args in (("quant_fp8", (x, 1, None, s, None)), ("quant_fp8", (x, 1, q, s, side)), ("quant_fp8", (x, 1.0, q, s, None)), ("quant_fp8", (x.float(), 1, q, s, None)),
+                    ("quant_fp8", (x, 128, q, s, None)), ("quant_fp8", (x, 1, q, s.t().contiguous().t(), None)), ("gemm_fp8", (q, s, *w["in"], None, None)),
+                    ("gemm_fp8", (q, s, *w["in"], wide, None)), ("gemm_fp8", (x, s, *w["in"], wide, None)), ("gemm_fp8", (q, s.half(), *w["in"], wide, None)),
+                    ("paged_append", (None, rows, rows, *z, st["cos"], st["sin"], st["Kc"], st["Vc"], st["Ks"], st["Vs"], None, False, None)),
+                    ("paged_append", (rows[:, :4], rows[:, 4:6], rows[:, 6:], z[0].long(), z[1], z[2], st["cos"], st["sin"], st["Kc"], st["Vc"], st["Ks"], st["Vs"], rows[:, :4].clone(), False, None)),
+                    ("paged_append", (rows[:, :4], rows[:, 4:6], rows[:, 6:], *z, st["cos"], st["sin"], st["Kc"], st["Vc"], None, None, rows[:, :4].clone(), False, None)),
+                    ("paged_attn_decode_fp8", (rows[:, :4], st["Kc"], st["Vc"], st["Ks"], st["Vs"], z[2], z[1], 0.1, rows[:, :4].clone(), None)),
+                    ("paged_attn_decode_fp8", (rows, st["Kc"], st["Vc"], st["Ks"], st["Vs"], z[2], z[1], 1, rows.clone(), None))):
+        assert native[f](*args) is None, f
+
+
+def test_binding_refuses_what_does_not_fit(lib):
+    w, st = layer_setup(lib, 3, 131)
+    x = rand((3, 384), BF16, 137).to(dev())
+    q, s = lib.mlt_quant_fp8(x)
+    rows = rand((3, 2, 64), BF16, 139).to(dev())
+    z, cs = st["where"], (st["cos"], st["sin"])
+    cache = (st["Kc"], st["Vc"], st["Ks"], st["Vs"])
+    for call in (lambda: lib.mlt_quant_fp8(x, Xq=q[:2]), lambda: lib.mlt_quant_fp8(x, S=s[:2]), lambda: lib.mlt_quant_fp8(x, S=s.double()), lambda: lib.mlt_quant_fp8(x.t()),
+                 lambda: lib.mlt_gemm_fp8(q, s[:2], *w["in"]), lambda: lib.mlt_gemm_fp8(q, s, *w["out"]), lambda: lib.mlt_gemm_fp8(q, s, *w["in"], C=x),
+                 lambda: lib.mlt_paged_append_fp8(None, rows, rows[:2], *z, *cs, *cache), lambda: lib.mlt_paged_append_fp8(None, rows, rows, z[0][:3], z[1], z[2], *cs, *cache),
+                 lambda: lib.mlt_paged_append_fp8(None, rows, rows, *z, cs[0], None, *cache), lambda: lib.mlt_paged_append_fp8(None, rows, rows, *z, *cs, *cache[:2], None, None),
+                 lambda: lib.mlt_paged_append_fp8(None, rows, rows, *z, *cs, cache[0], cache[1], cache[2][:3], cache[3]), lambda: lib.mlt_paged_append(None, rows, rows, *z, *cs, *cache[:2]),
+                 lambda: lib.mlt_paged_append_fp8(None, rows.transpose(0, 1).contiguous().transpose(0, 1), rows, *z, *cs, *cache),
+                 lambda: lib.mlt_paged_append_fp8(None, rows, rows, z[0].long(), z[1], z[2], *cs, *cache), lambda: lib.mlt_paged_append_fp8(None, rows, rows, *z, *cs, *cache, Qo=rows),
+                 lambda: lib.mlt_paged_attn_decode_fp8(rows, *cache, z[2], z[1][:2], 0.1), lambda: lib.mlt_paged_attn_decode_fp8(rows[:, :, :32], *cache, z[2], z[1], 0.1),
+                 lambda: lib.mlt_paged_attn_decode_fp8(rows, *cache[:2], cache[2].half(), cache[3], z[2], z[1], 0.1)):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+    with pytest.raises(TypeError):
+        lib.mlt_gemm_fp8(x, s, *w["in"])
+    with pytest.raises(TypeError):
+        lib.mlt_paged_attn_decode_fp8(rows, cache[0].float(), cache[1].float(), *cache[2:], z[2], z[1], 0.1)
+    with pytest.raises(lib.MltError) as e:
+        lib.mlt_paged_attn_decode_fp8(torch.cat([rows, rows[:, :1]], 1), *cache, z[2], z[1], 0.1)        # 3 query heads over 2
+    assert e.value.status == lib.MLT_ERR_INVALID_ARG
+    with pytest.raises(lib.MltError) as e:
+        lib.mlt_paged_append_fp8(None, rows, rows, *z, cs[0][:, :4].contiguous(), cs[1][:, :4].contiguous(), *cache)       # 8 turned elements
+    assert e.value.status == lib.MLT_ERR_UNSUPPORTED
+    with pytest.raises(lib.MltError) as e:
+        lib.mlt_quant_fp8(x, 64, Xq=torch.empty((3, 384), device=dev()).to(F8), S=torch.empty((3, 1), device=dev()))
+    assert e.value.status == lib.MLT_ERR_UNSUPPORTED
