@@ -78,6 +78,7 @@ int mlt_query_tiling(int op, const int64_t dims[4], int dtype, int32_t out[10]);
  * problem (alignment, shape) falls back to one that can, as the automatic choice would.
  *   gemm_variant  "general", "256", "256w8", "256pp16", "128pp16", "128pp16k128", "256x128kp", "224x128kp", "192x128kp", "160x128kp", "128kp", "256w4", "256w8x1",
  *                 "256w1x8", "128w8", "64x128", "64", "128k2", "64x128k2", "64k4", "skinny" (or its older name "skinnydma")
+ *                 mlt_gemm_fp8 has those of the names 256pp16, 128pp16, 256x128kp, 224x128kp, 192x128kp, 128kp and skinny, and its own choice for the others.
  *   mha_variant   "pp32", "pp16", "ps", "k2", "k4"
  * The initial values come from the environment variables MLT_GEMM_VARIANT and MLT_MHA_VARIANT,
  * which are read once, at the first call that needs them. Not synchronised with compute calls
@@ -91,13 +92,13 @@ int mlt_diag_force_variant(const char* gemm_variant, const char* mha_variant);
  * those with two K groups and the skinny kernel; partial products through an fp32 scratch, added in a fixed order by a second kernel,
  * in the skinny kernel by the workgroup that comes last): 0 = the
  * cost model's choice (the default), 1 = never split, 2 / 4 / 8 = that many parts, in the tile kernels wherever every
- * part keeps at least 8 K steps of 64. Process-wide, like mlt_diag_force_variant. Returns MLT_OK
+ * part keeps at least 8 K steps of 64 (mlt_gemm_fp8: in its kernels that can, whatever is left for a part). Process-wide, like mlt_diag_force_variant. Returns MLT_OK
  * or MLT_ERR_INVALID_ARG.
  */
 int mlt_diag_force_k_parts(int parts);
 
 /*
- * Number of key ranges per (sequence, head) that mlt_paged_attn_decode spreads over workgroups:
+ * Number of key ranges per (sequence, head) that mlt_paged_attn_decode and mlt_paged_attn_decode_fp8 spread over workgroups:
  * 0 = the library's choice (the default: by the CUs that sequences x heads leave idle and the
  * table's width; a batch, whose sequences differ in length, also with up to three pairs per CU),
  * 1..64 = that many (ranges beyond the end of a short sequence stay empty). The same for

@@ -12,6 +12,8 @@
 // the next step, and swaps between lane groups spread a row's scale over the four groups that hold its results (rows of A are the
 // columns of the MFMA, so a lane has one row a tile). Those loads sit in front of the step's direct ones, behind a wait for
 // all earlier ones: A of the next step has to have landed by the end of that phase anyway, and B has.
+#include <stdio.h>
+
 #include "fp8.h"
 #include "mlt_internal.h"
 
@@ -40,6 +42,78 @@ __device__ __forceinline__ void spread_groups(float x, float (&out)[4]) {
   out[3] = __builtin_bit_cast(float, (unsigned)b[1]);
 }
 
+// N blocks (8 tile rows of 128 bytes each) from `first` on, of a tile whose row 0 lies at gp (at this K step) and whose last row inside the matrix is `last`, into LDS:
+// lane l fetches the 16 bytes that belong at dst + 1024 i + 16 l, chunk (l & 7) ^ ((r >> 1) & 7) of row r. Rows past the matrix read its last rows again, chunks past
+// k_left (TAIL) the row's first; what lands there is never stored, or zeroed in the fragments. The lane's offset has two forms, for even and odd blocks; the rows go
+// into the scalar base: a load costs no vector instruction, which would stand in the memory phase's way (computed per load: 256 x 128 tiles 29 %
+// more time), and no register through the loop.
+// between(i) is called behind load i: the LDS reads of a memory phase go there, on a path of their own.
+template <int N, bool TAIL, typename Between>
+__device__ __forceinline__ void load_blocks(const char* gp, uint32_t ld, int last, int first, uint32_t dst, int lane, bool stream, int k_left, Between&& between) {
+  int ln = lane;
+  asm volatile("" : "+v"(ln));
+  uint32_t c0 = (uint32_t)((ln & 7) ^ (((ln >> 4) | (first << 2)) & 7)) * 16u, c1 = c0 ^ 64u;
+  if (TAIL) {
+    c0 = (int)c0 < k_left ? c0 : 0u;
+    c1 = (int)c1 < k_left ? c1 : 0u;
+  }
+  const uint32_t row = (uint32_t)(ln >> 3) * ld, v0 = row + c0, v1 = row + c1;
+  if ((first + N) * 8 - 1 <= last) {
+    const char* p = gp + (int64_t)(first * 8) * ld;
+    if (stream) {
+#pragma unroll
+      for (int i = 0; i < N; ++i, p += ld * 8) {
+        load_lds16_stream(p, i & 1 ? v1 : v0, dst + i * 1024);
+        between(i);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i, p += ld * 8) {
+        load_lds16(p, i & 1 ? v1 : v0, dst + i * 1024);
+        between(i);
+      }
+    }
+  } else {
+    const uint32_t edge = (uint32_t)((ln >> 3) < (last & 7) ? ln >> 3 : last & 7) * ld;
+    const int lb = last >> 3;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int b = first + i < lb ? first + i : lb;
+      load_lds16(gp + (int64_t)(b * 8) * ld, (b == lb ? edge : row) + (i & 1 ? c1 : c0), dst + i * 1024);
+      between(i);
+    }
+  }
+}
+
+// One K step of a wavefront's TA x TB tiles: the products of a scale block, and two MFMAs behind each its sum. now: the step's scales, row
+// 64 i + lane in now[i].
+// (One MFMA behind, a sum waits for its operand: 42 clocks an MFMA instead of 35, of which 32 are the MFMA's own. The empty asm
+// statements keep each MFMA and each sum where it is written: behind the last MFMA all parts would be alive.)
+template <int TA, int TB>
+__device__ __forceinline__ void mul_step(const u32x4 (&af)[2][TA], const u32x4 (&bf)[2][TB], const float (&now)[(TA + 3) / 4], f32x4 (&acc)[TA][TB]) {
+  f32x4 late[2];
+  float s[4], late_s[2] = {0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < TA * TB + 2; ++e) {
+    f32x4 part;
+    if (e < TA * TB) {
+      part = mfma16_e4m3(bf[0][e % TB], bf[1][e % TB], af[0][e / TB], af[1][e / TB], f32x4{0.f, 0.f, 0.f, 0.f});
+      asm volatile("" : "+v"(part));
+      __builtin_amdgcn_sched_barrier(0);
+      if (e % (4 * TB) == 0) spread_groups(now[e / (4 * TB)], s);
+    }
+    if (e > 1) {
+      f32x4& to = acc[(e - 2) / TB][(e - 2) % TB];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) to[r] += late[e & 1][r] * late_s[e & 1];
+      asm volatile("" : "+v"(to));
+    }
+    late[e & 1] = part;
+    late_s[e & 1] = s[e / TB % 4];
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
 }  // namespace
 
 // TAIL: K is no multiple of 128
@@ -59,51 +133,32 @@ __global__ __launch_bounds__(G8_NT, BT == 128 ? 4 : 1) void gemm_fp8_kernel(int 
   const int KT = (K + F8_KB - 1) / F8_KB;
   const int k_tail = K - (KT - 1) * F8_KB;               // TAIL: k values in the last step
 
-  // ---- global -> LDS: the wavefronts of group 1 fill the A tiles, those of group 0 the B tiles, NL blocks of 8 rows each. Row and
-  // offset of a lane are computed at each load: as registers they would not fit beside accumulators and fragments.
+  // ---- global -> LDS: the wavefronts of group 1 fill the A tiles, those of group 0 the B tiles, NL blocks of 8 rows each
   const char* ld_base = reinterpret_cast<const char*>(grp ? A + (int64_t)m0 * lda : B + (int64_t)n0 * ldb);
   const uint32_t ld_row = (uint32_t)(grp ? lda : ldb);
   const int ld_last = (grp ? M - m0 : N - n0) - 1;       // last row inside the matrix
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr_t)smem;
   const bool stream = grp == 1 ? nbn == 1 : nbm == 1;    // (read once: streaming form)
-  auto issue_loads = [&](int t, int slot) {
-    const char* gp = ld_base + (int64_t)t * F8_KB;
-    const uint32_t dst = lds0 + slot * SLOT + (wave & 3) * (NL * 1024);
-    int ln = lane;
-    asm volatile("" : "+v"(ln));                         // (not hoisted out of the loop)
-    const int r0 = (wave & 3) * NL * 8 + (ln >> 3);
-    uint32_t voff[NL];
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int r = r0 + 8 * i, rr = r < ld_last ? r : ld_last;
-      uint32_t c = (uint32_t)((ln & 7) ^ ((r >> 1) & 7)) * 16u;
-      if (TAIL && t == KT - 1 && (int)c >= k_tail) c = 0u;   // stays inside the matrix; zeroed in the fragments
-      voff[i] = (uint32_t)rr * ld_row + c;
-    }
-    if (stream) {
-#pragma unroll
-      for (int i = 0; i < NL; ++i) load_lds16_stream(gp, voff[i], dst + i * 1024);
-    } else {
-#pragma unroll
-      for (int i = 0; i < NL; ++i) load_lds16(gp, voff[i], dst + i * 1024);
-    }
+  auto issue_loads = [&](int t, int slot, auto&& between) __attribute__((always_inline)) {
+    load_blocks<NL, TAIL>(ld_base + (int64_t)t * F8_KB, ld_row, ld_last, (wave & 3) * NL, lds0 + slot * SLOT + (wave & 3) * (NL * 1024), lane, stream, K - t * F8_KB, between);
   };
+  auto nothing = [](int) __attribute__((always_inline)) {};
 
   // ---- scales: of row 64 i + lane of this wavefront's rows (with 64 rows: i = 0), and of the block of its columns
   constexpr int NS = WTM / 64;
-  int srow[NS];
+  uint32_t srow[NS];
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
     const int r = m0 + wm * WTM + 64 * i + lane;
-    srow[i] = r < M ? r : M - 1;
+    srow[i] = (uint32_t)(r < M ? r : M - 1);
   }
   const int ncol = n0 + wn * WTN < N ? n0 + wn * WTN : N - 1;
-  const float* sb_at = Sb + ncol / F8_KB;
+  const int scol = ncol / F8_KB;
   float sa[NS], sb;
   auto load_scales = [&](int t) {
 #pragma unroll
-    for (int i = 0; i < NS; ++i) sa[i] = Sa[(int64_t)t * ldsa + srow[i]];
-    sb = sb_at[(int64_t)t * ldsb];
+    for (int i = 0; i < NS; ++i) sa[i] = (Sa + (int64_t)t * ldsa)[srow[i]];
+    sb = (Sb + (int64_t)t * ldsb)[scol];
   };
 
   // ---- fragments: chunks h and 4 + h of a tile's rows
@@ -121,14 +176,11 @@ __global__ __launch_bounds__(G8_NT, BT == 128 ? 4 : 1) void gemm_fp8_kernel(int 
 #pragma unroll
     for (int j = 0; j < TB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   u32x4 af[2][TA], bf[2][TB];
-  auto read_frags = [&](const char* ta, const char* tb) {
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-#pragma unroll
-      for (int i = 0; i < TA; ++i) af[kk][i] = lds_read8<u32x4>(ta, a_off[kk] + i * 16 * F8_KB);
-#pragma unroll
-      for (int j = 0; j < TB; ++j) bf[kk][j] = lds_read8<u32x4>(tb, b_off[kk] + j * 16 * F8_KB);
-    }
+  // fragment f of 2 * (TA + TB): B's first, then A's in the order in which they are multiplied
+  auto read_frag = [&](const char* ta, const char* tb, int f) __attribute__((always_inline)) {
+    const int kk = f & 1, i = f >> 1;
+    if (i < TB) bf[kk][i] = lds_read8<u32x4>(tb, b_off[kk] + i * 16 * F8_KB);
+    else af[kk][i - TB] = lds_read8<u32x4>(ta, a_off[kk] + (i - TB) * 16 * F8_KB);
   };
   auto zero_tail = [&]() {                               // both operands: one alone would leave 0 * NaN
     const u32x4 zero4 = {0u, 0u, 0u, 0u};
@@ -149,8 +201,8 @@ __global__ __launch_bounds__(G8_NT, BT == 128 ? 4 : 1) void gemm_fp8_kernel(int 
   //   group 0, memory phase of step k (2k): issues B_{k+1} into the slot that A_{k-1} left in phase 2k-1, and waits for it at
   //     the end of its compute phase.
   load_scales(0);
-  issue_loads(0, grp ? 0 : 1);
-  if (KT > 1) { issue_loads(1, grp ? 2 : 3); __builtin_amdgcn_s_waitcnt(wait_imm(NL, 0)); }
+  issue_loads(0, grp ? 0 : 1, nothing);
+  if (KT > 1) { issue_loads(1, grp ? 2 : 3, nothing); __builtin_amdgcn_s_waitcnt(wait_imm(NL, 0)); }
   else __builtin_amdgcn_s_waitcnt(wait_imm(0, 0));
   MLT_BARRIER();
   if (grp == 1) MLT_BARRIER();
@@ -160,8 +212,6 @@ __global__ __launch_bounds__(G8_NT, BT == 128 ? 4 : 1) void gemm_fp8_kernel(int 
   for (int k = 0; k < KT; ++k) {
     const int slot_b = slot_a + 1 == G8_NSLOT ? 0 : slot_a + 1;
     // ---- memory phase
-    read_frags(smem + slot_a * SLOT, smem + slot_b * SLOT);
-    __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));          // group 1: A_{k+1}; both: the scales of step k
     __builtin_amdgcn_sched_barrier(0);
     float now[NS];                                        // this step's scales, row by lane
@@ -169,38 +219,26 @@ __global__ __launch_bounds__(G8_NT, BT == 128 ? 4 : 1) void gemm_fp8_kernel(int 
     for (int i = 0; i < NS; ++i) now[i] = sa[i] * sb;
     if (k + 1 < KT) load_scales(k + 1);
     __builtin_amdgcn_sched_barrier(0);
-    if (grp == 1) {
-      if (k + 2 < KT) issue_loads(k + 2, slot_a + 4 >= G8_NSLOT ? slot_a + 4 - G8_NSLOT : slot_a + 4);
+    const char *ta = smem + slot_a * SLOT, *tb = smem + slot_b * SLOT;
+    constexpr int NF = 2 * (TA + TB), PER = NF / NL;
+    static_assert(NF % NL == 0, "fragments behind each load");
+    const int next = grp == 1 ? (k + 2 < KT ? k + 2 : 0) : (k >= 1 && k + 1 < KT ? k + 1 : 0);
+    if (next) {
+      const int to = grp == 1 ? slot_a + 4 : slot_a + 3;
+      issue_loads(next, to >= G8_NSLOT ? to - G8_NSLOT : to, [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int f = 0; f < PER; ++f) read_frag(ta, tb, i * PER + f);
+      });
     } else {
-      if (k >= 1 && k + 1 < KT) issue_loads(k + 1, slot_a + 3 >= G8_NSLOT ? slot_a + 3 - G8_NSLOT : slot_a + 3);
+#pragma unroll
+      for (int f = 0; f < NF; ++f) read_frag(ta, tb, f);
     }
     __builtin_amdgcn_s_waitcnt(wait_imm(63, 0));
     if (TAIL && k == KT - 1) zero_tail();
     MLT_BARRIER();
     __builtin_amdgcn_sched_barrier(0);
     // ---- compute phase
-    // (the empty asm statements keep each MFMA and each sum where it is written: behind the last MFMA all parts would be alive)
-    f32x4 late;
-    float s[4], late_s = 0.f;
-#pragma unroll
-    for (int e = 0; e <= TA * TB; ++e) {
-      f32x4 part;
-      if (e < TA * TB) {
-        part = mfma16_e4m3(bf[0][e % TB], bf[1][e % TB], af[0][e / TB], af[1][e / TB], f32x4{0.f, 0.f, 0.f, 0.f});
-        asm volatile("" : "+v"(part));
-        __builtin_amdgcn_sched_barrier(0);
-        if (e % (4 * TB) == 0) spread_groups(now[e / (4 * TB)], s);
-      }
-      if (e > 0) {
-        f32x4& to = acc[(e - 1) / TB][(e - 1) % TB];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) to[r] += late[r] * late_s;
-        asm volatile("" : "+v"(to));
-      }
-      late = part;
-      late_s = s[e / TB % 4];
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    mul_step<TA, TB>(af, bf, now, acc);
     if (grp == 0) __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));
     MLT_BARRIER();
     __builtin_amdgcn_sched_barrier(0);
@@ -223,6 +261,196 @@ __global__ __launch_bounds__(G8_NT, BT == 128 ? 4 : 1) void gemm_fp8_kernel(int 
         for (int j = 0; j < TB; ++j)
           *reinterpret_cast<f32x4_mem*>(lds + (i * 16 + lq) * Rows::STRIDE + j * 16 + 4 * h) = acc[p * (RP / 16) + i][j];
     }, park, lane, m0 + wm * WTM + p * RP, n0 + wn * WTN, M, N, C, ldc, 0, nullptr);
+}
+
+namespace {
+
+// ---- the tiles of gemm_kp.hip: BM x 128, two groups of 4 wavefronts (2 x 2, BM/2 x 64 each) on alternate K steps, whose accumulators
+// are added through LDS at the end. Step s is read in phase s and multiplied in phase s + 1 by group s % 2. For grids that do not fill the chip with
+// 256 x 256 tiles: as many bytes of fragments per multiplication as there, and K may be split over workgroups (part_steps > 0), which
+// leave fp32 partial results.
+// A ring of R stages of one K step each (A tile, B tile, their scales); step s + R - 1 is fetched in phase s, by the group whose memory phase that is, into the
+// stage that the other one has read in phase s - 1. With R = 3 that is the group that will read it, which waits for it at the end of its compute phase, one phase
+// after the loads; with R = 4 it has two phases, and the wait stands at the end of the memory phase, behind the next loads. A phase of the
+// shorter tiles is less than the way from memory: R = 4 for them, what fits of the taller ones.
+template <int BM> struct K8Tile {
+  static constexpr int A_B = BM * F8_KB, B_B = 128 * F8_KB, S_B = 1024, STAGE = A_B + B_B + S_B;
+  static constexpr int R = 4 * STAGE <= 160 * 1024 ? 4 : 3;
+  static constexpr int NLA = A_B / 1024 / 4, NLB = B_B / 1024 / 4;       // 1 KB loads (8 rows) per wavefront of the group and step
+  static constexpr int NL = NLA + NLB + 1;                               // and one of scales
+  static constexpr int S = 128 + 4;                                      // floats per row of a group's image of the result
+  static constexpr int RPP = BM / 2;                                     // rows per pass of the epilogue
+  static constexpr int IMG_B = 2 * RPP * S * 4;
+  static constexpr int SMEM = R * STAGE > IMG_B ? R * STAGE : IMG_B;
+};
+
+}  // namespace
+
+template <typename Tag, int BM, bool TAIL>
+__global__ __launch_bounds__(G8_NT, 2) void gemm_fp8_kp_kernel(int M, int N, int K_, const uint8_t* __restrict__ A, int64_t lda, const float* __restrict__ Sa, int64_t ldsa,
+                                                               const uint8_t* __restrict__ B, int64_t ldb, const float* __restrict__ Sb, int64_t ldsb, uint16_t* __restrict__ C,
+                                                               int64_t ldc, int nbm, int nbn, int nxcd, int part_steps, float* __restrict__ part_out) {
+  typedef K8Tile<BM> T;
+  constexpr int R = T::R, NL = T::NL, NLA = T::NLA, NLB = T::NLB, WTM = BM / 2, WTN = 64, TA = WTM / 16, TB = WTN / 16;
+  extern __shared__ __align__(16) char smem[];
+  int K = K_, kb0 = 0;
+  const int tiles = nbm * nbn;
+  int logical, part = 0;
+  if (part_steps > 0) {                                  // an XCD takes the tiles of one part (one row of tiles: the same tiles of all parts)
+    if (nbm > 1) {
+      logical = logical_block(blockIdx.x, gridDim.x, nxcd);
+      part = logical / tiles;
+      logical -= part * tiles;
+    } else {
+      part = blockIdx.x / tiles;
+      logical = logical_block(blockIdx.x - part * tiles, tiles, nxcd);
+    }
+    kb0 = part * part_steps;
+    K = K_ - kb0 * F8_KB < part_steps * F8_KB ? K_ - kb0 * F8_KB : part_steps * F8_KB;   // > 0: the host launches no empty part
+  } else {
+    logical = logical_block(blockIdx.x, tiles, nxcd);
+  }
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = wave >> 2, w = wave & 3, wm = w >> 1, wn = w & 1;
+  int tile_m, tile_n;
+  tile_of_logical<G8_GROUP_M>(logical, nbm, nbn, tile_m, tile_n);
+  const int m0 = tile_m * BM, n0 = tile_n * 128;
+  const int KT = (K + F8_KB - 1) / F8_KB;
+  const int k_tail = K - (KT - 1) * F8_KB;
+
+  // ---- global -> LDS: wavefront w of a group fills blocks w * NLA .. of A and w * NLB .. of B of a step, and 64 scales: those of the rows 64 w .. of the
+  // tile (past its end: never read); the columns' scale comes by a scalar load
+  const char* const a_base = reinterpret_cast<const char*>(A + (int64_t)m0 * lda) + (int64_t)kb0 * F8_KB;
+  const char* const b_base = reinterpret_cast<const char*>(B + (int64_t)n0 * ldb) + (int64_t)kb0 * F8_KB;
+  const int a_last = M - 1 - m0, b_last = N - 1 - n0;
+  const bool stream_a = nbn == 1, stream_b = nbm == 1;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr_t)smem;
+  const uint32_t srow = (uint32_t)((m0 + 64 * w + lane < M ? m0 + 64 * w + lane : M - 1) * 4);
+  auto issue = [&](int s, int stage, auto&& between) __attribute__((always_inline)) {
+    const uint32_t at = lds0 + stage * T::STAGE;
+    load_lds4(Sa + (int64_t)(kb0 + s) * ldsa, srow, at + T::A_B + T::B_B + w * 256);
+    load_blocks<NLA, TAIL>(a_base + (int64_t)s * F8_KB, (uint32_t)lda, a_last, w * NLA, at + w * (NLA * 1024), lane, stream_a, K - s * F8_KB, between);
+    load_blocks<NLB, TAIL>(b_base + (int64_t)s * F8_KB, (uint32_t)ldb, b_last, w * NLB, at + T::A_B + w * (NLB * 1024), lane, stream_b, K - s * F8_KB,
+                           [&](int i) __attribute__((always_inline)) { between(NLA + i); });
+  };
+  auto nothing = [](int) __attribute__((always_inline)) {};
+  constexpr int NS = (WTM + 63) / 64;
+  const float* sb_at = Sb + tile_n;                      // (128 columns: one block)
+
+  const int lq = lane & 15, h = lane >> 4, swz = (lq >> 1) & 7;
+  int a_off[2], b_off[2];
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+    a_off[kk] = (wm * WTM + lq) * F8_KB + (((4 * kk + h) ^ swz) * 16);
+    b_off[kk] = T::A_B + (wn * WTN + lq) * F8_KB + (((4 * kk + h) ^ swz) * 16);
+  }
+  f32x4 acc[TA][TB];
+#pragma unroll
+  for (int i = 0; i < TA; ++i)
+#pragma unroll
+    for (int j = 0; j < TB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  u32x4 af[2][TA], bf[2][TB];
+
+  // the steps before R - 1, as if fetched in the phases before 0
+  constexpr bool OWN = R % 2 == 1;                        // a group fetches the steps that it reads
+#pragma unroll
+  for (int j = 0; j < R - 1; ++j)
+    if (((j - (R - 1)) & 1) == grp && j < KT) issue(j, j, nothing);
+  // step 0 has to have landed at the first barrier: of its group's loads only those of step 2 may be in flight
+  if (!OWN && KT > 2 && grp == 1) __builtin_amdgcn_s_waitcnt(wait_imm(NL, 15));
+  else if (grp == (OWN ? 0 : 1)) __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));
+  MLT_BARRIER();
+  if (grp == 1) {
+    if (OWN) __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));
+    MLT_BARRIER();
+  }
+  int stage = grp;
+  int ld_stage = (grp + R - 1) % R;                       // of step s + R - 1
+#pragma clang loop unroll(disable)
+  for (int s = grp; s < KT; s += 2) {
+    // ---- memory phase s
+    const char* st = smem + stage * T::STAGE;
+    const float sb = sb_at[(int64_t)(kb0 + s) * ldsb];
+    float now[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) now[i] = reinterpret_cast<const f32_mem*>(st + T::A_B + T::B_B)[wm * WTM + 64 * i + lane];
+    constexpr int NF = 2 * (TA + TB);
+    auto read_frag = [&](int f) __attribute__((always_inline)) {
+      const int kk = f & 1, i = f >> 1;
+      if (i < TB) bf[kk][i] = lds_read8<u32x4>(st, b_off[kk] + i * 16 * F8_KB);
+      else af[kk][i - TB] = lds_read8<u32x4>(st, a_off[kk] + (i - TB) * 16 * F8_KB);
+    };
+    if (s + R - 1 < KT) {
+      issue(s + R - 1, ld_stage, [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int f = i * NF / (NL - 1); f < (i + 1) * NF / (NL - 1); ++f) read_frag(f);
+      });
+      if (!OWN) __builtin_amdgcn_s_waitcnt(wait_imm(NL, 15));   // step s + 1, fetched two phases ago
+    } else {
+#pragma unroll
+      for (int f = 0; f < NF; ++f) read_frag(f);
+      if (!OWN) __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));
+    }
+    __builtin_amdgcn_s_waitcnt(wait_imm(63, 0));
+#pragma unroll
+    for (int i = 0; i < NS; ++i) now[i] *= sb;
+    if (TAIL && s == KT - 1) {
+      const u32x4 zero4 = {0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+        if ((4 * kk + h) * 16 >= k_tail) {
+#pragma unroll
+          for (int i = 0; i < TA; ++i) af[kk][i] = zero4;
+#pragma unroll
+          for (int j = 0; j < TB; ++j) bf[kk][j] = zero4;
+        }
+    }
+    MLT_BARRIER();
+    __builtin_amdgcn_sched_barrier(0);
+    // ---- compute phase s + 1
+    mul_step<TA, TB>(af, bf, now, acc);
+    if (OWN) __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));
+    MLT_BARRIER();
+    __builtin_amdgcn_sched_barrier(0);
+    stage = stage + 2 >= R ? stage + 2 - R : stage + 2;
+    ld_stage = ld_stage + 2 >= R ? ld_stage + 2 - R : ld_stage + 2;
+  }
+  if ((KT & 1) == grp) MLT_BARRIER();                     // KT + 1 phases for both groups
+
+  // ---- epilogue: RPP rows at a time both groups park their accumulators in images of their own; all threads add the two
+  float* const img = reinterpret_cast<float*>(smem);
+  constexpr int S = T::S, RPP = T::RPP;
+#pragma unroll
+  for (int p = 0; p < BM / RPP; ++p) {
+    if (p > 0) __syncthreads();
+    if (wm == p) {
+      float* mine = img + (grp * RPP + lq) * S + wn * WTN + 4 * h;
+#pragma unroll
+      for (int i = 0; i < TA; ++i)
+#pragma unroll
+        for (int j = 0; j < TB; ++j) *reinterpret_cast<f32x4_mem*>(mine + i * 16 * S + j * 16) = acc[i][j];
+    }
+    __syncthreads();
+    const int row0 = m0 + p * RPP;
+    if (part_steps > 0) {
+      for (int e = tid; e < RPP * 32; e += G8_NT) {
+        const int r = e / 32, c = e % 32 * 4;
+        f32x4 v = *reinterpret_cast<const f32x4_mem*>(img + r * S + c);
+        add4(v, *reinterpret_cast<const f32x4_mem*>(img + (RPP + r) * S + c));
+        if (row0 + r < M && n0 + c < N) store_row4(v, part_out + ((int64_t)part * M + row0 + r) * N + n0 + c, N - n0 - c, false);
+      }
+    } else {
+      for (int e = tid; e < RPP * 16; e += G8_NT) {
+        const int r = e / 16, c = e % 16 * 8;
+        const float* src = img + r * S + c;
+        f32x4 lo = *reinterpret_cast<const f32x4_mem*>(src), hi = *reinterpret_cast<const f32x4_mem*>(src + 4);
+        add4(lo, *reinterpret_cast<const f32x4_mem*>(src + RPP * S));
+        add4(hi, *reinterpret_cast<const f32x4_mem*>(src + RPP * S + 4));
+        if (row0 + r < M && n0 + c < N) store_row8<Tag, false>(lo, hi, C + (int64_t)(row0 + r) * ldc + n0 + c, N - n0 - c, 0, nullptr);
+      }
+    }
+  }
 }
 
 namespace {
@@ -253,43 +481,128 @@ int run_fp8_tile(const GemmFp8Args& a, hipStream_t s) {
   return a.K % F8_KB ? launch_fp8<Tag, BT, true>(a, s) : launch_fp8<Tag, BT, false>(a, s);
 }
 
+template <typename Tag, int BM, bool TAIL>
+int launch_fp8_kp(const GemmFp8Args& a, int parts, float* part, hipStream_t s) {
+  constexpr int SMEM = K8Tile<BM>::SMEM;
+  auto kern = gemm_fp8_kp_kernel<Tag, BM, TAIL>;
+  static thread_local int configured_dev = -1;
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return MLT_ERR_DEVICE;
+  if (configured_dev != dev) {
+    if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, SMEM) != hipSuccess) {
+      (void)hipGetLastError();
+      return MLT_ERR_LAUNCH;
+    }
+    configured_dev = dev;
+  }
+  const int64_t nbm = (a.M + BM - 1) / BM, nbn = (a.N + 127) / 128;
+  if (nbm * nbn * parts > 0x7fffffff) return MLT_ERR_UNSUPPORTED;
+  const int KT = (int)((a.K + F8_KB - 1) / F8_KB), part_steps = parts > 1 ? (KT + parts - 1) / parts : 0;
+  if (parts > 1) parts = (KT + part_steps - 1) / part_steps;                // no empty part
+  hipLaunchKernelGGL(kern, dim3((unsigned)(nbm * nbn * parts)), dim3(G8_NT), SMEM, s, (int)a.M, (int)a.N, (int)a.K, a.A, a.lda, a.Sa, a.ldsa, a.B, a.ldb, a.Sb, a.ldsb, a.C,
+                     a.ldc, (int)nbm, (int)nbn, device_xcds(), part_steps, part);
+  if (hipGetLastError() != hipSuccess) return MLT_ERR_LAUNCH;
+  if (part_steps == 0) return MLT_OK;
+  GemmArgs g{a.M, a.N, a.K, nullptr, 0, nullptr, 0, 1, a.C, a.ldc, a.dtype, GEMM_AUTO, 0};
+  g.scratch = part;
+  return run_splitk_reduce(g, parts, a.M * a.N, s);
+}
+
+template <typename Tag, int BM>
+int run_fp8_kp(const GemmFp8Args& a, int parts, float* part, hipStream_t s) {
+  return a.K % F8_KB ? launch_fp8_kp<Tag, BM, true>(a, parts, part, s) : launch_fp8_kp<Tag, BM, false>(a, parts, part, s);
+}
+
 __global__ void zero_rows_kernel(uint16_t* __restrict__ C, int64_t ldc, int M, int N) {
   for (int64_t e = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; e < (int64_t)M * N; e += (int64_t)gridDim.x * blockDim.x) C[e / N * ldc + e % N] = 0;
 }
 
+// Estimated time (us) of a kernel on ncu CUs, fitted to 260 shapes of 65 to 4096 rows (rms of the error 6 %; the choice by it costs 0.6 % on average against
+// the best of them): a launch, then rounds of workgroups over the chip, each round its K steps (slower the more of the chip is busy: delivery from the L2s, power) and
+// a prologue and epilogue; writing C; with K in parts writing and adding up the partial results.
+// us per step and tile: 256 x 256 1.18 to 1.48, 256 x 128 0.79 to 0.91, 128 x 128 0.56 to 0.62 and, two to a CU, 1.09 for both.
+// The kernel for few rows (fitted to 90 shapes): B at the memory's rate, A at what a CU takes, once for each group of columns.
+double fp8_estimate(int variant, int parts, int64_t M, int64_t N, int64_t K, int64_t ncu) {
+  if (variant == GEMM_SKINNY) {
+    const int64_t rows = (M + 15) / 16 * 16, cols = (N * parts + ncu - 1) / ncu, per_group = rows <= 32 ? 128 : 64, groups = (cols + per_group - 1) / per_group;
+    return 2.2 + 2.0 * groups + (double)N * K / 6.7e6 + (double)rows * K * groups / parts / 95e3 + (parts > 1 ? 0.9 + 1.1e-5 * N * rows : 0.0);
+  }
+  const int64_t KT = (K + F8_KB - 1) / F8_KB, steps = (KT + parts - 1) / parts;
+  const double mb = (double)M * N * 1e-6;                // of elements of C
+  auto tiles = [&](int64_t bm, int64_t bn) { return (M + bm - 1) / bm * ((N + bn - 1) / bn) * ((KT + steps - 1) / steps); };
+  if (variant == GEMM_128_PP16) {                        // two workgroups per CU; up to ncu of them, one each
+    const int64_t w = tiles(128, 128), full = w / (2 * ncu), rest = w % (2 * ncu);
+    const int64_t both = full + (rest > ncu ? 1 : 0), one = rest > 0 && rest <= ncu ? 1 : 0;
+    return 3.35 + steps * (1.09 * both + 0.77 * one) + 0.28 * (both + one) + 0.38 * mb;
+  }
+  struct Cost { int64_t bm, bn; double step, fill, launch, round; };
+  const Cost c = variant == GEMM_256_PP16 ? Cost{256, 256, 1.18, 0.305, 1.6, 5.6}
+               : variant == GEMM_256X128_KP ? Cost{256, 128, 0.79, 0.125, 2.8, 4.8}
+               : variant == GEMM_224X128_KP ? Cost{224, 128, 0.75, 0.09, 3.2, 3.7}
+               : variant == GEMM_192X128_KP ? Cost{192, 128, 0.69, 0.07, 3.0, 3.6} : Cost{128, 128, 0.56, 0.06, 2.6, 3.3};
+  const int64_t w = tiles(c.bm, c.bn), rounds = (w + ncu - 1) / ncu;
+  return c.launch + steps * (c.step * rounds + c.fill * w / ncu) + c.round * rounds + 0.3 * mb + (parts > 1 ? 3.3 + 1.4 * parts * mb : 0.0);
+}
+
+struct Fp8Plan { int variant, parts; };
+
+Fp8Plan plan_fp8(const GemmFp8Args& a, int max_parts, int64_t ncu) {
+  static const int tall[] = {GEMM_256X128_KP, GEMM_224X128_KP, GEMM_192X128_KP, GEMM_128_KP};
+  auto known = [&](int v) { return v == GEMM_256_PP16 || v == GEMM_128_PP16 || v == tall[0] || v == tall[1] || v == tall[2] || v == tall[3] || (v == GEMM_SKINNY && a.M <= 64); };
+  const int forced = known(a.forced) ? a.forced : GEMM_AUTO;
+  Fp8Plan best{forced == GEMM_AUTO ? GEMM_256_PP16 : forced, 1};
+  double least = 1e30;
+  auto offer = [&](int v, int parts) {
+    if (forced != GEMM_AUTO && v != forced) return;
+    const double t = fp8_estimate(v, parts, a.M, a.N, a.K, ncu);
+    if (t < least) { least = t; best = Fp8Plan{v, parts}; }
+  };
+  for (int parts = 1; parts <= max_parts; parts *= 2) {
+    if (a.forced_parts > 0 ? parts != a.forced_parts && max_parts > 1 : parts > 1 && (parts * a.M * a.N * 4 > kStaticScratchBytes || a.K < 256 * parts)) continue;
+    for (int v : tall) offer(v, parts);
+    if (a.M <= 64 && (parts <= 2 || a.forced_parts > 0)) offer(GEMM_SKINNY, parts);
+  }
+  if (a.forced_parts <= 1 || max_parts == 1 || best.parts == 1) {
+    offer(GEMM_256_PP16, 1);
+    offer(GEMM_128_PP16, 1);
+  }
+  return best;
+}
+
 template <typename Tag>
-int run_fp8_t(const GemmFp8Args& a, hipStream_t s, const char** name) {
+int run_fp8_t(const GemmFp8Args& a, hipStream_t s, char* name, size_t size) {
   if (a.K == 0) {
-    *name = "gemm_fp8_zero";
+    snprintf(name, size, "gemm_fp8_zero");
     hipLaunchKernelGGL(zero_rows_kernel, dim3(1024), dim3(256), 0, s, a.C, a.ldc, (int)a.M, (int)a.N);
     return hipGetLastError() == hipSuccess ? MLT_OK : MLT_ERR_LAUNCH;
   }
   DeviceInfo di;
   const int64_t ncu = device_info(di) && di.ncu > 0 ? di.ncu : 256;
-  if (a.M <= 64) {
-    int parts = a.forced_parts > 1 ? a.forced_parts : 1;
-    float* part = nullptr;
-    if (parts > 1) {
-      part = cached_scratch(parts * a.M * a.N * (int64_t)sizeof(float), s);
-      if (!part) parts = 1;
-    }
-    static const char* const names[9] = {"", "gemm_fp8_skinny", "gemm_fp8_skinny_splitk2", "", "gemm_fp8_skinny_splitk4", "", "", "", "gemm_fp8_skinny_splitk8"};
-    *name = names[parts];
-    return run_gemm_fp8_skinny(a, parts, part, s);
+  Fp8Plan p = plan_fp8(a, 8, ncu);
+  float* part = nullptr;
+  if (p.parts > 1) {
+    part = cached_scratch(p.parts * a.M * a.N * (int64_t)sizeof(float), s);
+    if (!part) p = plan_fp8(a, 1, ncu);                  // no scratch to be had: the best of the plain forms
   }
-  const int64_t big = ((a.M + 255) / 256) * ((a.N + 255) / 256);
-  if (big >= ncu) {
-    *name = "gemm_fp8_256x256";
-    return run_fp8_tile<Tag, 256>(a, s);
+  const char* tile = p.variant == GEMM_SKINNY ? "skinny" : p.variant == GEMM_256_PP16 ? "256x256_pp" : p.variant == GEMM_128_PP16 ? "128x128_pp" : p.variant == GEMM_256X128_KP ? "256x128_kp"
+                   : p.variant == GEMM_224X128_KP ? "224x128_kp" : p.variant == GEMM_192X128_KP ? "192x128_kp" : "128x128_kp";
+  if (p.parts > 1) snprintf(name, size, "gemm_fp8_%s_splitk%d", tile, p.parts);
+  else snprintf(name, size, "gemm_fp8_%s", tile);
+  switch (p.variant) {
+    case GEMM_SKINNY: return run_gemm_fp8_skinny(a, p.parts, part, s);
+    case GEMM_256_PP16: return run_fp8_tile<Tag, 256>(a, s);
+    case GEMM_128_PP16: return run_fp8_tile<Tag, 128>(a, s);
+    case GEMM_256X128_KP: return run_fp8_kp<Tag, 256>(a, p.parts, part, s);
+    case GEMM_224X128_KP: return run_fp8_kp<Tag, 224>(a, p.parts, part, s);
+    case GEMM_192X128_KP: return run_fp8_kp<Tag, 192>(a, p.parts, part, s);
   }
-  *name = "gemm_fp8_128x128";
-  return run_fp8_tile<Tag, 128>(a, s);
+  return run_fp8_kp<Tag, 128>(a, p.parts, part, s);
 }
 
 }  // namespace
 
-int run_gemm_fp8(const GemmFp8Args& a, hipStream_t s, const char** name) {
-  return a.dtype == MLT_BF16 ? run_fp8_t<bf16_tag>(a, s, name) : run_fp8_t<f16_tag>(a, s, name);
+int run_gemm_fp8(const GemmFp8Args& a, hipStream_t s, char* name, size_t size) {
+  return a.dtype == MLT_BF16 ? run_fp8_t<bf16_tag>(a, s, name, size) : run_fp8_t<f16_tag>(a, s, name, size);
 }
 
 }  // namespace mlt

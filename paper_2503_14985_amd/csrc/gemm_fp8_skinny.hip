@@ -24,11 +24,6 @@ constexpr int S8_KP = 256;            // k values per piece
 constexpr int S8_RING = 20 * 1024;    // LDS ring of a wavefront
 constexpr int S8_SMEM = S8_NW * S8_RING;
 
-// A dword per lane from its own address straight into LDS at lds_addr + 4 * lane
-__device__ __forceinline__ void load_lds4(const void* p, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_addr), "v"(p) : "memory", "m0");
-}
-
 // MT: 16-row tiles of A. AU, BU: load instructions (4 rows each) for a piece of a row tile, of a column block: 4, or fewer where no more rows
 // or columns exist
 template <int MT, int AU, int BU> struct S8Cfg {

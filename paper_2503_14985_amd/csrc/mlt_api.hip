@@ -385,15 +385,18 @@ int mlt_gemm_fp8(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, co
     if (256 * (lda > ldb ? lda : ldb) >= ((int64_t)1 << 31)) return MLT_ERR_UNSUPPORTED;   // 32-bit offsets inside a tile
   }
   if (!device_is_gfx950()) return MLT_ERR_DEVICE;
-  GemmFp8Args a{M, N, K, (const uint8_t*)A, lda, Sa, ldsa, (const uint8_t*)B, ldb, Sb, ldsb, (uint16_t*)C, ldc, dtype, overrides().gemm_parts};
+  GemmFp8Args a{M, N, K, (const uint8_t*)A, lda, Sa, ldsa, (const uint8_t*)B, ldb, Sb, ldsb, (uint16_t*)C, ldc, dtype, forced_gemm_variant(), overrides().gemm_parts};
   hipStream_t s = (hipStream_t)stream;
-  const char* name = "";
+  char name[sizeof g_name_buf];
   int rc;
   {
     TimedRegion t(s);
-    rc = run_gemm_fp8(a, s, &name);
+    rc = run_gemm_fp8(a, s, name, sizeof name);
   }
-  if (rc == MLT_OK) g_last_kernel = name;
+  if (rc == MLT_OK) {
+    memcpy(g_name_buf, name, sizeof name);
+    g_last_kernel = g_name_buf;
+  }
   return rc;
 }
 

@@ -199,10 +199,10 @@ struct GemmFp8Args {
   const float* Sb; int64_t ldsb;
   uint16_t* C; int64_t ldc;
   int dtype;
-  int forced_parts = 0;      // as in GemmArgs
+  int forced = GEMM_AUTO, forced_parts = 0;   // as in GemmArgs; of the variants those that exist here: 256pp16, 128pp16, 256x128kp, 224x128kp, 192x128kp, 128kp, skinny
 };
 int run_gemm_fp8_skinny(const GemmFp8Args& a, int parts, float* part, hipStream_t s);   // gemm_fp8_skinny.hip: M <= 64; part: parts * M * N floats behind their counters
-int run_gemm_fp8(const GemmFp8Args& a, hipStream_t s, const char** name);   // gemm_fp8.hip
+int run_gemm_fp8(const GemmFp8Args& a, hipStream_t s, char* name, size_t size);   // gemm_fp8.hip; name: of the kernel that ran
 struct AppendArgs {
   int64_t T, B, Hq, H, D, block_size, max_blocks, num_blocks;
   const uint16_t* Q; int64_t ldq;

@@ -110,7 +110,8 @@ def test_oracle_against_torch():
     back = q * np.repeat(np.repeat(s.T, 128, 0)[:130], 128, 1)[:, :200]
     assert (np.abs(back - x) <= 2.0 ** -4 * np.abs(x) + 2.0 ** -10 * s.max()).all()
     a, sa = u.quant(g.standard_normal((5, 200)), 1)
-    c, _ = u.gemm(a, sa, q, s)
+    c, mass, top = u.gemm(a, sa, q, s)
+    assert (np.abs(c) <= mass * (1 + 1e-12)).all() and (top <= mass).all() and (mass <= 8 * top * (1 + 1e-12)).all()
     assert np.allclose(c, (a * np.repeat(sa.T, 128, 1)[:, :200]) @ back.T, rtol=1e-12, atol=1e-12)
     z = g.standard_normal((3, 2, 8))
     t = g.uniform(-3, 3, (3, 4))

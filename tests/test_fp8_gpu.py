@@ -96,9 +96,8 @@ def gemm_operands(M, N, K, seed):
 
 
 def gemm_check(C, a, sa, b, sb, dtype, K):
-    ref, mass = u.gemm(f64(a), f64(sa), f64(b), f64(sb))
-    # K products and as many fp32 additions, a scale's product and the scaled block's rounding each; then the output's
-    tol = u.HALF[dtype] * np.abs(ref) + mass * (K + 4 * sa.shape[0]) * 2.0 ** -24 * 1.01 + 2.0 ** -25
+    ref, mass, top = u.gemm(f64(a), f64(sa), f64(b), f64(sb))
+    tol = u.gemm_tolerance(ref, mass, top, K, sa.shape[0], dtype)
     if dtype == FP16:
         assert np.abs(ref).max() < 6e4
     err = np.abs(f64(C) - ref)
@@ -138,15 +137,74 @@ def k_parts(lib):
     lib.mlt_diag_force_k_parts(0)
 
 
+TILES = {"256pp16": "256x256_pp", "128pp16": "128x128_pp", "256x128kp": "256x128_kp", "224x128kp": "224x128_kp", "192x128kp": "192x128_kp", "128kp": "128x128_kp"}
+
+
+@pytest.fixture
+def variant(lib):
+    yield lambda v: lib.mlt_diag_force_variant(gemm=v)
+    lib.mlt_diag_force_variant(gemm="auto")
+
+
+@pytest.mark.parametrize("name", sorted(TILES))
+@pytest.mark.parametrize("M,N,K", [(1, 5, 128), (70, 200, 16), (129, 300, 272), (255, 129, 384), (256, 256, 512), (300, 777, 1040), (513, 640, 640), (900, 1030, 1296)])
+def test_gemm_every_tile_kernel(lib, variant, name, M, N, K):
+    """Tiles with rows and columns past the matrix, one K step, an odd and an even number of them, a step that K does not fill."""
+    variant(name)
+    a, sa, b, sb = gemm_operands(M, N, K, M + N + K)
+    for dtype in (BF16, FP16):
+        C = torch.full((M, N + 3), -7.0, dtype=dtype, device=dev())
+        lib.mlt_gemm_fp8(a.to(dev()), sa.to(dev()), b.to(dev()), sb.to(dev()), C=C[:, :N])
+        assert lib.mlt_last_kernel().startswith("gemm_fp8_" + TILES[name]), lib.mlt_last_kernel()
+        gemm_check(C[:, :N], a, sa, b, sb, dtype, K)
+        assert bool((C[:, N:] == -7.0).all())
+
+
+def test_gemm_plan_follows_the_shape(lib):
+    """The choice by itself: few rows stream B, a full grid takes the large tiles, few tiles against a long K its split, none of it under capture."""
+    def name(M, N, K):
+        a, b = (torch.zeros((r, K), device=dev()).to(F8) for r in (M, N))
+        lib.mlt_gemm_fp8(a, torch.ones((-(-K // 128), M), device=dev()), b, torch.ones((-(-K // 128), -(-N // 128)), device=dev()))
+        return lib.mlt_last_kernel()
+    assert name(16, 4096, 4096) == "gemm_fp8_skinny"
+    assert name(64, 512, 14336) == "gemm_fp8_skinny_splitk2"
+    assert name(64, 28672, 14336) == "gemm_fp8_128x128_kp"
+    assert name(4096, 4096, 4096) == "gemm_fp8_256x256_pp"
+    assert name(2048, 4096, 1024) == "gemm_fp8_128x128_pp"
+    assert "_splitk" in name(128, 1024, 14336)
+    assert name(7, 9, 0) == "gemm_fp8_zero"
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = name(128, 1024, 14336)
+    assert captured.startswith("gemm_fp8_") and "_splitk" not in captured
+
+
+@pytest.mark.parametrize("parts", [2, 4, 8])
+@pytest.mark.parametrize("name", [n for n in sorted(TILES) if n.endswith("kp")])
+def test_gemm_tiles_with_k_in_parts(lib, variant, k_parts, name, parts):
+    """Parts of one step and of several, of an odd number, the last one shorter; added in a fixed order."""
+    variant(name)
+    k_parts(parts)
+    for M, N, K in ((100, 130, 1024), (300, 520, 3216), (257, 128, 128 * parts)):
+        a, sa, b, sb = gemm_operands(M, N, K, M + N + K + parts)
+        at = [t.to(dev()) for t in (a, sa, b, sb)]
+        C = lib.mlt_gemm_fp8(*at)
+        assert lib.mlt_last_kernel() == "gemm_fp8_%s_splitk%d" % (TILES[name], parts)
+        gemm_check(C, a, sa, b, sb, BF16, K)
+        for _ in range(3):
+            assert torch.equal(lib.mlt_gemm_fp8(*at).view(torch.int16), C.view(torch.int16))
+
+
 @pytest.mark.parametrize("parts", [2, 4, 8])
 @pytest.mark.parametrize("M,N,K", [(1, 64, 128), (3, 1030, 2048), (16, 4096, 4112), (30, 520, 1040), (64, 2000, 2304), (50, 5000, 1024)])
-def test_gemm_k_split_across_workgroups(lib, k_parts, parts, M, N, K):
-    """Parts of K by workgroups of their own, some of them empty, added by the last one; the same bits on every run."""
+def test_gemm_k_split_across_workgroups(lib, k_parts, variant, parts, M, N, K):
+    """Few rows: parts of K by workgroups of their own, some of them empty, added by the last one; the same bits on every run."""
     k_parts(parts)
+    variant("skinny")
     a, sa, b, sb = gemm_operands(M, N, K, M + N + K + parts)
     at = [t.to(dev()) for t in (a, sa, b, sb)]
     C = lib.mlt_gemm_fp8(*at)
-    assert lib.mlt_last_kernel().endswith("_splitk%d" % parts)
+    assert lib.mlt_last_kernel() == "gemm_fp8_skinny_splitk%d" % parts
     gemm_check(C, a, sa, b, sb, BF16, K)
     for _ in range(4):
         assert torch.equal(lib.mlt_gemm_fp8(*at).view(torch.int16), C.view(torch.int16))
