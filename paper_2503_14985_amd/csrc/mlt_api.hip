@@ -433,18 +433,19 @@ int mlt_paged_attn_decode_fp8(int64_t B, int64_t Hq, int64_t H, int64_t D, int64
   if (!aligned(Q, 16) || !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(O, 2) || !aligned(Ks, 4) || !aligned(Vs, 4) || !aligned(block_table, 4) ||
       !aligned(seq_lens, 4)) return MLT_ERR_INVALID_ARG;
   if (B > INT_MAX || Hq > INT_MAX || B * Hq > INT_MAX || max_blocks > INT_MAX || max_blocks * block_size > INT_MAX || num_blocks > INT_MAX) return MLT_ERR_UNSUPPORTED;
+  if (num_blocks * H > INT_MAX || num_blocks * H * (block_size / 16) > INT_MAX) return MLT_ERR_UNSUPPORTED;   // units of 16 rows are counted in 32 bits
   if (!device_is_gfx950()) return MLT_ERR_DEVICE;
   PagedFp8Args a{B, Hq, H, D, block_size, max_blocks, num_blocks, (const uint16_t*)Q, (const uint8_t*)Kc, (const uint8_t*)Vc, Ks, Vs, block_table,
                  seq_lens, (uint16_t*)O, scale, dtype, overrides().key_split};
   hipStream_t s = (hipStream_t)stream;
-  int rc, nsplit = 1;
+  int rc, nsplit = 1, waves = 4;
   {
     TimedRegion t(s);
-    rc = run_paged_fp8(a, s, &nsplit);
+    rc = run_paged_fp8(a, s, &nsplit, &waves);
   }
   if (rc == MLT_OK) {
-    if (nsplit > 1) snprintf(g_name_buf, sizeof g_name_buf, "paged_decode_fp8_d%d_w4_keysplit%d", (int)D, nsplit);
-    else snprintf(g_name_buf, sizeof g_name_buf, "paged_decode_fp8_d%d_w4", (int)D);
+    if (nsplit > 1) snprintf(g_name_buf, sizeof g_name_buf, "paged_decode_fp8_d%d_w%d_keysplit%d", (int)D, waves, nsplit);
+    else snprintf(g_name_buf, sizeof g_name_buf, "paged_decode_fp8_d%d_w%d", (int)D, waves);
     g_last_kernel = g_name_buf;
   }
   return rc;

@@ -229,7 +229,7 @@ struct PagedFp8Args {
   int dtype;
   int forced_split = 0;      // as in PagedArgs
 };
-int run_paged_fp8(const PagedFp8Args& a, hipStream_t s, int* nsplit_out);   // paged_fp8.hip
+int run_paged_fp8(const PagedFp8Args& a, hipStream_t s, int* nsplit_out, int* waves_out);   // paged_fp8.hip; key ranges per pair and wavefronts per workgroup that ran
 
 // The library's own scratch memory for a stream of the current device: at least `bytes`, behind its counters, kept
 // (and grown by doubling) from call to call, never freed; nullptr if it cannot be had, and while the

@@ -474,7 +474,7 @@ def key_split(lib):
 def test_attn_key_split(lib, key_split, nsplit, dtype, D):
     key_split(nsplit)
     at, O = attn_case(lib, [1, 0, 2, 16, 33, 257, 1023, 2048, 3001], 6, 2, D, 16, dtype, 53)
-    assert lib.mlt_last_kernel().endswith("_keysplit%d" % nsplit if nsplit > 1 else "w4")
+    assert lib.mlt_last_kernel().endswith("_keysplit%d" % nsplit if nsplit > 1 else "_w8")
     for _ in range(3):
         assert torch.equal(lib.mlt_paged_attn_decode_fp8(*at, 1.0 / math.sqrt(D)), O)
 
@@ -484,6 +484,18 @@ def test_attn_long_and_batches(lib):
     assert "keysplit" in lib.mlt_last_kernel()
     attn_case(lib, [100 + 3 * i for i in range(70)], 8, 8, 64, 16, FP16, 61, poison=False)
     attn_case(lib, [1 + 40 * i for i in range(40)], 8, 2, 128, 32, BF16, 67, poison=False)
+
+
+@pytest.mark.parametrize("H,Hq,D,top,nsplit", [(16, 16, 128, 1030, 1), (40, 40, 64, 2050, 1), (5, 90, 128, 2050, 2), (16, 16, 128, 1030, 3)])
+def test_attn_mixed_batch_dealt_by_length(lib, key_split, H, Hq, D, top, nsplit):
+    """Enough workgroups, and enough for each to read, for them to be dealt out by length: equal lengths, empty sequences and a negative length among them."""
+    key_split(nsplit)
+    lens = [0, 7, 1000, 7, 7, top, 0, 64, 65, 96, 96, 1, 500, 1000, 31, 33, 800, 0, 2]
+    at, O = attn_case(lib, lens, Hq, H, D, 32, BF16, 79, poison=False)
+    low = at[6].clone()
+    low[low == 0] = -9
+    for _ in range(3):
+        assert torch.equal(lib.mlt_paged_attn_decode_fp8(*at[:6], low, 1.0 / math.sqrt(D)), O)
 
 
 def test_attn_single_key_and_constant_values(lib):
