@@ -2,7 +2,7 @@
 //   C[m][n] = sum over blocks kb of Sa[kb][m] * Sb[kb][n / 128] * sum over k in kb of A[m][k] * B[n][k]
 // One MFMA (16x16x128) multiplies a block's 128 k of a 16 x 16 tile; its fp32 result, started from zero, goes into the fp32
 // accumulator with the product of the two scales. That is four fused multiply-adds behind each MFMA of 32 clocks, which take 16 clocks of
-// the vector unit beside it: they are issued one MFMA late, while the next one runs.
+// the vector unit beside it: they are issued two MFMAs late, while later ones run.
 //
 // The schedule is that of gemm_pp.hip, whose K step of 64 16-bit values has the bytes of a K step of 128 here: workgroup tile 256 x 256
 // (or 128 x 128, two workgroups per CU), 8 wavefronts as 2 x 4, the two of a SIMD half a step apart, one refilling its
@@ -521,14 +521,21 @@ __global__ void zero_rows_kernel(uint16_t* __restrict__ C, int64_t ldc, int M, i
 // the best of them): a launch, then rounds of workgroups over the chip, each round its K steps (slower the more of the chip is busy: delivery from the L2s, power) and
 // a prologue and epilogue; writing C; with K in parts writing and adding up the partial results.
 // us per step and tile: 256 x 256 1.18 to 1.48, 256 x 128 0.79 to 0.91, 128 x 128 0.56 to 0.62 and, two to a CU, 1.09 for both.
-// The kernel for few rows (fitted to 90 shapes): B at the memory's rate, A at what a CU takes, once for each group of columns.
+// The kernel for few rows (fitted to 650 shapes of 1 to 1024 rows, rms 9 %; the choice among all of them costs 0.8 % on average): B from memory, once for each row of
+// workgroups; A at what a CU takes, 85 bytes a ns, once for each group of columns. It wins where a matrix is too small for a tile on every CU: 128 x 1024 x 4096 8.1 us, by
+// 128 x 128 tiles and 8 parts of K 13.0; 512 x 512 x 1024 5.0 and 9.5; 1024 x 1024 x 1024 8.7 and 9.7.
 double fp8_estimate(int variant, int parts, int64_t M, int64_t N, int64_t K, int64_t ncu) {
+  const double mb = (double)M * N * 1e-6;                // of elements of C
   if (variant == GEMM_SKINNY) {
-    const int64_t rows = (M + 15) / 16 * 16, cols = (N * parts + ncu - 1) / ncu, per_group = rows <= 32 ? 128 : 64, groups = (cols + per_group - 1) / per_group;
-    return 2.2 + 2.0 * groups + (double)N * K / 6.7e6 + (double)rows * K * groups / parts / 95e3 + (parts > 1 ? 0.9 + 1.1e-5 * N * rows : 0.0);
+    // as gemm_fp8_skinny.hip lays it out: z rows of workgroups, `rows` of C each; cols columns a workgroup, in groups; rounds of workgroups; what one reads of A and B (KB)
+    const int64_t rows = gemm_fp8_skinny_rows(M), z = (M + rows - 1) / rows, per = z * parts, wide = ncu > per ? ncu / per : 1, nwg = N < wide ? N : wide, cols = (N + nwg - 1) / nwg;
+    const int64_t cb = gemm_skinny_cols(N, parts, ncu / z), padded = rows <= 4 ? 4 : (rows + 15) / 16 * 16, pieces = ((K + 255) / 256 + parts - 1) / parts;
+    const double groups = (double)((cols + (padded <= 32 ? 127 : 63)) / (padded <= 32 ? 128 : 64)), rounds = (double)((nwg * per + ncu - 1) / ncu), nk = (double)N * K * 1e-6;
+    const double k = (pieces * 256 < K ? pieces * 256 : K) * 1e-3, a = padded * k, b = (cols + cb - 1) / cb * cb * k;
+    return 1.9 + 0.013 * nk + 0.021 * z * nk + 1.28 * mb + rounds * (groups * (2.0 + 0.0118 * a + 0.18 * ((pieces + 7) / 8)) + 0.0185 * b) +
+           (parts > 1 ? 0.9 + parts * (0.21 + 3.0 * mb + 1.4e-4 * cols * rows * rounds) : 0.0);
   }
   const int64_t KT = (K + F8_KB - 1) / F8_KB, steps = (KT + parts - 1) / parts;
-  const double mb = (double)M * N * 1e-6;                // of elements of C
   auto tiles = [&](int64_t bm, int64_t bn) { return (M + bm - 1) / bm * ((N + bn - 1) / bn) * ((KT + steps - 1) / steps); };
   if (variant == GEMM_128_PP16) {                        // two workgroups per CU; up to ncu of them, one each
     const int64_t w = tiles(128, 128), full = w / (2 * ncu), rest = w % (2 * ncu);
@@ -541,14 +548,14 @@ double fp8_estimate(int variant, int parts, int64_t M, int64_t N, int64_t K, int
                : variant == GEMM_224X128_KP ? Cost{224, 128, 0.75, 0.09, 3.2, 3.7}
                : variant == GEMM_192X128_KP ? Cost{192, 128, 0.69, 0.07, 3.0, 3.6} : Cost{128, 128, 0.56, 0.06, 2.6, 3.3};
   const int64_t w = tiles(c.bm, c.bn), rounds = (w + ncu - 1) / ncu;
-  return c.launch + steps * (c.step * rounds + c.fill * w / ncu) + c.round * rounds + 0.3 * mb + (parts > 1 ? 3.3 + 1.4 * parts * mb : 0.0);
+  return c.launch + steps * (c.step * rounds + c.fill * w / ncu) + c.round * rounds + 0.3 * mb + (parts > 1 ? 2.5 + parts * (0.2 + 1.4 * mb) : 0.0);
 }
 
 struct Fp8Plan { int variant, parts; };
 
 Fp8Plan plan_fp8(const GemmFp8Args& a, int max_parts, int64_t ncu) {
   static const int tall[] = {GEMM_256X128_KP, GEMM_224X128_KP, GEMM_192X128_KP, GEMM_128_KP};
-  auto known = [&](int v) { return v == GEMM_256_PP16 || v == GEMM_128_PP16 || v == tall[0] || v == tall[1] || v == tall[2] || v == tall[3] || (v == GEMM_SKINNY && a.M <= 64); };
+  auto known = [&](int v) { return v == GEMM_256_PP16 || v == GEMM_128_PP16 || v == tall[0] || v == tall[1] || v == tall[2] || v == tall[3] || (v == GEMM_SKINNY && a.M <= GEMM_FP8_FEW_ROWS); };
   const int forced = known(a.forced) ? a.forced : GEMM_AUTO;
   Fp8Plan best{forced == GEMM_AUTO ? GEMM_256_PP16 : forced, 1};
   double least = 1e30;
@@ -560,7 +567,7 @@ Fp8Plan plan_fp8(const GemmFp8Args& a, int max_parts, int64_t ncu) {
   for (int parts = 1; parts <= max_parts; parts *= 2) {
     if (a.forced_parts > 0 ? parts != a.forced_parts && max_parts > 1 : parts > 1 && (parts * a.M * a.N * 4 > kStaticScratchBytes || a.K < 256 * parts)) continue;
     for (int v : tall) offer(v, parts);
-    if (a.M <= 64 && (parts <= 2 || a.forced_parts > 0)) offer(GEMM_SKINNY, parts);
+    if (a.M <= GEMM_FP8_FEW_ROWS && parts <= 8) offer(GEMM_SKINNY, parts);
   }
   if (a.forced_parts <= 1 || max_parts == 1 || best.parts == 1) {
     offer(GEMM_256_PP16, 1);
@@ -578,7 +585,7 @@ int run_fp8_t(const GemmFp8Args& a, hipStream_t s, char* name, size_t size) {
   }
   DeviceInfo di;
   const int64_t ncu = device_info(di) && di.ncu > 0 ? di.ncu : 256;
-  Fp8Plan p = plan_fp8(a, 8, ncu);
+  Fp8Plan p = plan_fp8(a, 16, ncu);
   float* part = nullptr;
   if (p.parts > 1) {
     part = cached_scratch(p.parts * a.M * a.N * (int64_t)sizeof(float), s);

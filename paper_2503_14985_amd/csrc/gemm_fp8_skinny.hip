@@ -1,4 +1,4 @@
-// mlt_gemm_fp8 with few rows (M <= 64, next-token decode): the design of gemm_skinny.hip on e4m3 operands. The cost is reading B once:
+// mlt_gemm_fp8 with few rows (next-token decode) or little work: the design of gemm_skinny.hip on e4m3 operands. The cost is reading B once:
 // one workgroup of 8 wavefronts per CU, each with its share of the columns (rows of the stored B) in blocks of up to 16; the
 // wavefronts split K in pieces of 256 k, 256 bytes a row and two scale blocks. Every wavefront fetches its pieces of A and B
 // straight into an LDS ring of its own, several slots ahead, waits for the oldest by count and multiplies: two MFMAs of 128 k for a piece of
@@ -10,7 +10,10 @@
 // group of columns is at most 128 wide and so touches two).
 //
 // With few columns a CU fetches more of A than of B; K may then be split over 2, 4 or 8 workgroups (PARTS), whose fp32 partial results
-// the one that comes last at a counter adds in the order of the parts.
+// the one that comes last at a counter adds in the order of the parts. More than 64 rows are shared out to rows of workgroups (blockIdx.z), which read B once
+// each: a matrix too small to give every CU a tile of 128 x 128 is better off with 64 x 16 and no barrier in the loop over K.
+//
+// Measured: 16 x 4096 x 4096 5.0 us, 24 x 14336 x 4096 12.4 us (59 MB, 4.8 TB/s), 65 x 8192 x 1024 7.3 us, 512 x 512 x 1024 5.0 us.
 #include "fp8.h"
 #include "mlt_internal.h"
 
@@ -38,7 +41,7 @@ template <int MT, int AU, int BU> struct S8Cfg {
 };
 
 struct S8 {
-  int M, N, K, share, rest, lda, ldb;
+  int M, N, K, rows, share, rest, lda, ldb;
   const uint8_t *A, *B;
   const float *Sa, *Sb;
   int64_t ldsa, ldsb;
@@ -53,7 +56,12 @@ __global__ __launch_bounds__(S8_NT, 2) void gemm_fp8_skinny_kernel(S8 a) {
   typedef S8Cfg<MT, AU, BU> L;
   constexpr int CB = L::CB, R = L::R;
   extern __shared__ __align__(16) char smem[];
-  const int M = a.M, N = a.N, K = a.K;
+  const int m0 = (int)blockIdx.z * a.rows, M = a.M - m0 < a.rows ? a.M - m0 : a.rows, N = a.N, K = a.K;   // this workgroup's rows
+  const uint8_t* const A = a.A + (int64_t)m0 * (uint32_t)a.lda;
+  const float* const Sa = a.Sa + m0;
+  uint16_t* const C = a.C + (int64_t)m0 * a.ldc;
+  const int64_t part_size = (int64_t)a.M * N;
+  float* const part = PARTS ? a.part + (int64_t)m0 * N : nullptr;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, q = lane >> 4;
@@ -87,7 +95,7 @@ __global__ __launch_bounds__(S8_NT, 2) void gemm_fp8_skinny_kernel(S8 a) {
     const int nblock0 = (c0 + base * CB) / 128, nblock_last = (N - 1) / 128;
     // where this lane's scales lie: rows of A (less 16 * row tile) or a block of columns, and which of a piece's two k blocks
     const int nblock = nblock0 + (lane & 1) < nblock_last ? nblock0 + (lane & 1) : nblock_last;
-    const float* sp = lane < 32 ? a.Sa : a.Sb + nblock;
+    const float* sp = lane < 32 ? Sa : a.Sb + nblock;
     const int64_t sld = lane < 32 ? a.ldsa : a.ldsb;
     const int skb = lane < 32 ? lane >> 4 : (lane >> 1) & 1;
     f32x4 acc[GB][MT];
@@ -107,8 +115,9 @@ __global__ __launch_bounds__(S8_NT, 2) void gemm_fp8_skinny_kernel(S8 a) {
       // rows past the matrix (past this workgroup's columns) and chunks past K: the piece's first chunk for all such
       // lanes, never stored or zeroed later; the instruction stays, and with it the count of loads in flight
       if (f_s < MT) {
-        const char* src = reinterpret_cast<const char*>(a.A + (int64_t)(f_s * 16) * (uint32_t)a.lda + k0);
+        // (the last workgroups' rows may end before a row tile: then all lanes read the first row's chunk)
         const int rows = M - f_s * 16;
+        const char* src = reinterpret_cast<const char*>(A + (int64_t)(rows > 0 ? f_s * 16 : 0) * (uint32_t)a.lda + k0);
 #pragma unroll
         for (int i = 0; i < AU; ++i) {
           const int row = i * 4 + lane / 16;
@@ -233,8 +242,8 @@ __global__ __launch_bounds__(S8_NT, 2) void gemm_fp8_skinny_kernel(S8 a) {
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < S8_NW; ++w) sum += reinterpret_cast<const float*>(smem)[w * (S8_RING / 4) + e];
-        if (PARTS) store_shared(a.part + ((int64_t)blockIdx.y * M + gr) * N + gc, sum);
-        else a.C[(int64_t)gr * a.ldc + gc] = Elem<Tag>::from_f32(sum);
+        if (PARTS) store_shared(part + (int64_t)blockIdx.y * part_size + (int64_t)gr * N + gc, sum);
+        else C[(int64_t)gr * a.ldc + gc] = Elem<Tag>::from_f32(sum);
       }
     }
     if (base + GB < nblk) __syncthreads();
@@ -243,7 +252,7 @@ __global__ __launch_bounds__(S8_NT, 2) void gemm_fp8_skinny_kernel(S8 a) {
 
   // the last part of these columns to get here adds them all (EB elements of a thread at a time, all their parts requested
   // before the first is used: each such round is a trip to memory)
-  if (!last_to_arrive(a.counter + bid, gridDim.y, reinterpret_cast<uint32_t*>(smem))) return;
+  if (!last_to_arrive(a.counter + blockIdx.z * gridDim.x + bid, gridDim.y, reinterpret_cast<uint32_t*>(smem))) return;
   const int cols = c1 - c0, parts = (int)gridDim.y;
   constexpr int EB = MT == 1 ? 2 : 4;
   for (int e0 = tid; e0 < M * cols; e0 += EB * S8_NT) {
@@ -258,7 +267,7 @@ __global__ __launch_bounds__(S8_NT, 2) void gemm_fp8_skinny_kernel(S8 a) {
     for (int p = 0; p < 8; ++p)
       if (p < parts) {
 #pragma unroll
-        for (int i = 0; i < EB; ++i) v[p][i] = load_shared(a.part + (int64_t)p * M * N + at[i]);
+        for (int i = 0; i < EB; ++i) v[p][i] = load_shared(part + p * part_size + at[i]);
       }
 #pragma unroll
     for (int p = 1; p < 8; ++p)
@@ -270,13 +279,13 @@ __global__ __launch_bounds__(S8_NT, 2) void gemm_fp8_skinny_kernel(S8 a) {
     for (int i = 0; i < EB; ++i)
       if (e0 + i * S8_NT < M * cols) {
         const int gr = (e0 + i * S8_NT) / cols, gc = c0 + (e0 + i * S8_NT) % cols;
-        a.C[(int64_t)gr * a.ldc + gc] = Elem<Tag>::from_f32(v[0][i]);
+        C[(int64_t)gr * a.ldc + gc] = Elem<Tag>::from_f32(v[0][i]);
       }
   }
 }
 
 template <typename Tag, int MT, int AU, int BU, bool PARTS, int GB>
-int launch_s8_blocks(const GemmFp8Args& g, int parts, float* part, unsigned nwg, hipStream_t s) {
+int launch_s8_blocks(const GemmFp8Args& g, int rows, int parts, float* part, unsigned nwg, hipStream_t s) {
   auto kern = gemm_fp8_skinny_kernel<Tag, MT, AU, BU, PARTS, GB>;
   static thread_local int configured_dev = -1;            // opt in to > 64 KB LDS once per device
   int dev = 0;
@@ -288,41 +297,42 @@ int launch_s8_blocks(const GemmFp8Args& g, int parts, float* part, unsigned nwg,
     }
     configured_dev = dev;
   }
-  S8 a{(int)g.M, (int)g.N, (int)g.K, (int)(g.N / nwg), (int)(g.N % nwg), (int)g.lda, (int)g.ldb, g.A, g.B, g.Sa, g.Sb, g.ldsa, g.ldsb, g.C, g.ldc, part,
+  S8 a{(int)g.M, (int)g.N, (int)g.K, rows, (int)(g.N / nwg), (int)(g.N % nwg), (int)g.lda, (int)g.ldb, g.A, g.B, g.Sa, g.Sb, g.ldsa, g.ldsb, g.C, g.ldc, part,
        PARTS ? scratch_counters(part) : nullptr};
-  hipLaunchKernelGGL(kern, dim3(nwg, (unsigned)parts), dim3(S8_NT), S8_SMEM, s, a);
+  hipLaunchKernelGGL(kern, dim3(nwg, (unsigned)parts, (unsigned)((g.M + rows - 1) / rows)), dim3(S8_NT), S8_SMEM, s, a);
   return hipGetLastError() == hipSuccess ? MLT_OK : MLT_ERR_LAUNCH;
 }
 
 template <typename Tag, int MT, int AU, int BU, bool PARTS>
-int launch_s8(const GemmFp8Args& g, int parts, float* part, int64_t ncu, hipStream_t s) {
+int launch_s8(const GemmFp8Args& g, int rows, int parts, float* part, int64_t ncu, hipStream_t s) {
   constexpr int MAX_GB = S8Cfg<MT, AU, BU>::MAX_GB;
-  const int64_t want = ncu / parts > 0 ? ncu / parts : 1;
+  const int64_t per = parts * ((g.M + rows - 1) / rows), want = ncu / per > 0 ? ncu / per : 1;
   const unsigned nwg = (unsigned)(g.N < want ? g.N : want);   // one workgroup per CU, every one with columns
   const int64_t blocks = ((g.N + nwg - 1) / nwg + 4 * BU - 1) / (4 * BU);
-  if (blocks == 1) return launch_s8_blocks<Tag, MT, AU, BU, PARTS, 1>(g, parts, part, nwg, s);
-  if (blocks == 2 && MAX_GB == 8) return launch_s8_blocks<Tag, MT, AU, BU, PARTS, MAX_GB == 8 ? 2 : MAX_GB>(g, parts, part, nwg, s);
-  return launch_s8_blocks<Tag, MT, AU, BU, PARTS, MAX_GB>(g, parts, part, nwg, s);
+  if (blocks == 1) return launch_s8_blocks<Tag, MT, AU, BU, PARTS, 1>(g, rows, parts, part, nwg, s);
+  if (blocks == 2 && MAX_GB == 8) return launch_s8_blocks<Tag, MT, AU, BU, PARTS, MAX_GB == 8 ? 2 : MAX_GB>(g, rows, parts, part, nwg, s);
+  return launch_s8_blocks<Tag, MT, AU, BU, PARTS, MAX_GB>(g, rows, parts, part, nwg, s);
 }
 
 template <typename Tag, int MT, int AU>
-int run_s8_cols(const GemmFp8Args& g, int parts, float* part, int64_t ncu, hipStream_t s) {
-  if (parts > 1) return launch_s8<Tag, MT, AU, 4, true>(g, parts, part, ncu, s);
-  switch (gemm_skinny_cols(g.N, parts, ncu)) {
-    case 4: return launch_s8<Tag, MT, AU, 1, false>(g, 1, nullptr, ncu, s);
-    case 8: return launch_s8<Tag, MT, AU, 2, false>(g, 1, nullptr, ncu, s);
+int run_s8_cols(const GemmFp8Args& g, int rows, int parts, float* part, int64_t ncu, hipStream_t s) {
+  if (parts > 1) return launch_s8<Tag, MT, AU, 4, true>(g, rows, parts, part, ncu, s);
+  switch (gemm_skinny_cols(g.N, parts, ncu / ((g.M + rows - 1) / rows))) {
+    case 4: return launch_s8<Tag, MT, AU, 1, false>(g, rows, 1, nullptr, ncu, s);
+    case 8: return launch_s8<Tag, MT, AU, 2, false>(g, rows, 1, nullptr, ncu, s);
   }
-  return launch_s8<Tag, MT, AU, 4, false>(g, 1, nullptr, ncu, s);
+  return launch_s8<Tag, MT, AU, 4, false>(g, rows, 1, nullptr, ncu, s);
 }
 
 template <typename Tag>
 int run_s8_t(const GemmFp8Args& g, int parts, float* part, int64_t ncu, hipStream_t s) {
-  if (g.M <= 4) return run_s8_cols<Tag, 1, 1>(g, parts, part, ncu, s);
-  switch ((g.M + 15) / 16) {
-    case 1: return run_s8_cols<Tag, 1, 4>(g, parts, part, ncu, s);
-    case 2: return run_s8_cols<Tag, 2, 4>(g, parts, part, ncu, s);
-    case 3: return run_s8_cols<Tag, 3, 4>(g, parts, part, ncu, s);
-    case 4: return run_s8_cols<Tag, 4, 4>(g, parts, part, ncu, s);
+  const int rows = gemm_fp8_skinny_rows(g.M);
+  if (rows <= 4) return run_s8_cols<Tag, 1, 1>(g, rows, parts, part, ncu, s);
+  switch ((rows + 15) / 16) {
+    case 1: return run_s8_cols<Tag, 1, 4>(g, rows, parts, part, ncu, s);
+    case 2: return run_s8_cols<Tag, 2, 4>(g, rows, parts, part, ncu, s);
+    case 3: return run_s8_cols<Tag, 3, 4>(g, rows, parts, part, ncu, s);
+    case 4: return run_s8_cols<Tag, 4, 4>(g, rows, parts, part, ncu, s);
   }
   return MLT_ERR_UNSUPPORTED;
 }

@@ -167,15 +167,16 @@ def test_gemm_plan_follows_the_shape(lib):
         lib.mlt_gemm_fp8(a, torch.ones((-(-K // 128), M), device=dev()), b, torch.ones((-(-K // 128), -(-N // 128)), device=dev()))
         return lib.mlt_last_kernel()
     assert name(16, 4096, 4096) == "gemm_fp8_skinny"
-    assert name(64, 512, 14336) == "gemm_fp8_skinny_splitk2"
+    assert name(64, 512, 14336).startswith("gemm_fp8_skinny_splitk")
+    assert name(512, 512, 1024) == "gemm_fp8_skinny"
     assert name(64, 28672, 14336) == "gemm_fp8_128x128_kp"
     assert name(4096, 4096, 4096) == "gemm_fp8_256x256_pp"
     assert name(2048, 4096, 1024) == "gemm_fp8_128x128_pp"
-    assert "_splitk" in name(128, 1024, 14336)
+    assert name(512, 1024, 16384).startswith("gemm_fp8_128x128_kp_splitk")
     assert name(7, 9, 0) == "gemm_fp8_zero"
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        captured = name(128, 1024, 14336)
+        captured = name(512, 1024, 16384)
     assert captured.startswith("gemm_fp8_") and "_splitk" not in captured
 
 
@@ -208,6 +209,22 @@ def test_gemm_k_split_across_workgroups(lib, k_parts, variant, parts, M, N, K):
     gemm_check(C, a, sa, b, sb, BF16, K)
     for _ in range(4):
         assert torch.equal(lib.mlt_gemm_fp8(*at).view(torch.int16), C.view(torch.int16))
+
+
+@pytest.mark.parametrize("parts", [1, 2, 8])
+@pytest.mark.parametrize("M", [65, 80, 129, 200, 333, 777, 1000, 1024])
+def test_gemm_rows_shared_out(lib, k_parts, variant, parts, M):
+    """More rows than one workgroup of the kernel for few rows takes: the last share ends inside a tile of 16 or before one; operands without a byte behind them."""
+    k_parts(parts)
+    variant("skinny")
+    for N, K, dtype in ((1, 16, BF16), (150, 528, FP16), (40, 4112, BF16)):
+        a, sa, b, sb = gemm_operands(M, N, K, M + N + K + parts)
+        at = [t.to(dev()) for t in (a, sa, b, sb)]
+        C = torch.full((M + 2, N), 7.0, dtype=dtype, device=dev())
+        lib.mlt_gemm_fp8(*at, C=C[1:-1])
+        assert lib.mlt_last_kernel() == "gemm_fp8_skinny" + ("_splitk%d" % parts if parts > 1 else "")
+        assert bool((C[0] == 7).all()) and bool((C[-1] == 7).all())
+        gemm_check(C[1:-1], a, sa, b, sb, dtype, K)
 
 
 def test_gemm_large_sampled(lib):
