@@ -521,9 +521,9 @@ __global__ void zero_rows_kernel(uint16_t* __restrict__ C, int64_t ldc, int M, i
 // the best of them): a launch, then rounds of workgroups over the chip, each round its K steps (slower the more of the chip is busy: delivery from the L2s, power) and
 // a prologue and epilogue; writing C; with K in parts writing and adding up the partial results.
 // us per step and tile: 256 x 256 1.18 to 1.48, 256 x 128 0.79 to 0.91, 128 x 128 0.56 to 0.62 and, two to a CU, 1.09 for both.
-// The kernel for few rows (fitted to 650 shapes of 1 to 1024 rows, rms 9 %; the choice among all of them costs 0.8 % on average): B from memory, once for each row of
-// workgroups; A at what a CU takes, 85 bytes a ns, once for each group of columns. It wins where a matrix is too small for a tile on every CU: 128 x 1024 x 4096 8.1 us, by
-// 128 x 128 tiles and 8 parts of K 13.0; 512 x 512 x 1024 5.0 and 9.5; 1024 x 1024 x 1024 8.7 and 9.7.
+// The kernel for few rows (fitted to 1000 shapes of 1 to 4096 rows, rms 10 % up to 64 rows and 7 % above; the choice among all kernels costs 1 % on average): B from memory,
+// A and B at what a CU takes, 50 to 130 bytes a ns, A once for each group of columns, and the wavefronts' turns at pieces of K. It wins where a matrix is too small for
+// a tile on every CU: 128 x 1024 x 4096 8.1 us, by 128 x 128 tiles and 8 parts of K 13.0; 512 x 512 x 1024 5.0 and 9.5; 1024 x 1024 x 1024 8.7 and 9.7.
 double fp8_estimate(int variant, int parts, int64_t M, int64_t N, int64_t K, int64_t ncu) {
   const double mb = (double)M * N * 1e-6;                // of elements of C
   if (variant == GEMM_SKINNY) {
@@ -531,9 +531,11 @@ double fp8_estimate(int variant, int parts, int64_t M, int64_t N, int64_t K, int
     const int64_t rows = gemm_fp8_skinny_rows(M), z = (M + rows - 1) / rows, per = z * parts, wide = ncu > per ? ncu / per : 1, nwg = N < wide ? N : wide, cols = (N + nwg - 1) / nwg;
     const int64_t cb = gemm_skinny_cols(N, parts, ncu / z), padded = rows <= 4 ? 4 : (rows + 15) / 16 * 16, pieces = ((K + 255) / 256 + parts - 1) / parts;
     const double groups = (double)((cols + (padded <= 32 ? 127 : 63)) / (padded <= 32 ? 128 : 64)), rounds = (double)((nwg * per + ncu - 1) / ncu), nk = (double)N * K * 1e-6;
-    const double k = (pieces * 256 < K ? pieces * 256 : K) * 1e-3, a = padded * k, b = (cols + cb - 1) / cb * cb * k;
-    return 1.9 + 0.013 * nk + 0.021 * z * nk + 1.28 * mb + rounds * (groups * (2.0 + 0.0118 * a + 0.18 * ((pieces + 7) / 8)) + 0.0185 * b) +
-           (parts > 1 ? 0.9 + parts * (0.21 + 3.0 * mb + 1.4e-4 * cols * rows * rounds) : 0.0);
+    const double k = (pieces * 256 < K ? pieces * 256 : K) * 1e-3, a = padded * k, b = (cols + cb - 1) / cb * cb * k, turns = (double)((pieces + 7) / 8), tile = (double)cols * rows;
+    if (z == 1)
+      return 2.27 + 0.053 * nk + groups * (1.98 + 0.0124 * a + 0.067 * turns) + 0.0142 * b + 0.78 * mb + (parts > 1 ? 0.73 + parts * (0.15 + 3.46 * mb + 1.2e-4 * tile) : 0.0);
+    return 3.16 + rounds * (groups * (0.34 + 0.0064 * a + 1.07 * turns) + 0.0218 * b) + 2.96 * mb +
+           (parts > 1 ? 1.29 * ((cols * rows + 2047) / 2048) + parts * (0.3 + 1.58 * mb + 1.4e-4 * tile * rounds) : 0.0);
   }
   const int64_t KT = (K + F8_KB - 1) / F8_KB, steps = (KT + parts - 1) / parts;
   auto tiles = [&](int64_t bm, int64_t bn) { return (M + bm - 1) / bm * ((N + bn - 1) / bn) * ((KT + steps - 1) / steps); };

@@ -10,7 +10,7 @@
 // group of columns is at most 128 wide and so touches two).
 //
 // With few columns a CU fetches more of A than of B; K may then be split over 2, 4 or 8 workgroups (PARTS), whose fp32 partial results
-// the one that comes last at a counter adds in the order of the parts. More than 64 rows are shared out to rows of workgroups (blockIdx.z), which read B once
+// the one that comes last at a counter adds in the order of the parts. More than 64 rows are shared out to rows of workgroups, which read B once
 // each: a matrix too small to give every CU a tile of 128 x 128 is better off with 64 x 16 and no barrier in the loop over K.
 //
 // Measured: 16 x 4096 x 4096 5.0 us, 24 x 14336 x 4096 12.4 us (59 MB, 4.8 TB/s), 65 x 8192 x 1024 7.3 us, 512 x 512 x 1024 5.0 us.
@@ -41,7 +41,7 @@ template <int MT, int AU, int BU> struct S8Cfg {
 };
 
 struct S8 {
-  int M, N, K, rows, share, rest, lda, ldb;
+  int M, N, K, rows, share, rest, lda, ldb, nz, nxcd;
   const uint8_t *A, *B;
   const float *Sa, *Sb;
   int64_t ldsa, ldsb;
@@ -56,7 +56,17 @@ __global__ __launch_bounds__(S8_NT, 2) void gemm_fp8_skinny_kernel(S8 a) {
   typedef S8Cfg<MT, AU, BU> L;
   constexpr int CB = L::CB, R = L::R;
   extern __shared__ __align__(16) char smem[];
-  const int m0 = (int)blockIdx.z * a.rows, M = a.M - m0 < a.rows ? a.M - m0 : a.rows, N = a.N, K = a.K;   // this workgroup's rows
+  // share of the columns, of the rows, part of K. With several shares of the rows an XCD gets all of them for neighbouring columns of one part (777 x 2048 x 8192: 43 us,
+  // 53 with the columns in turn)
+  int bid = (int)blockIdx.x, z = 0, part_id = (int)blockIdx.y;
+  if (a.nz > 1) {
+    const int width = (int)gridDim.x, l = logical_block(bid + part_id * width, width * (int)gridDim.y, a.nxcd);
+    part_id = PARTS ? l / width : 0;
+    const int at = l - part_id * width;
+    bid = at / a.nz;
+    z = at - bid * a.nz;
+  }
+  const int m0 = z * a.rows, M = a.M - m0 < a.rows ? a.M - m0 : a.rows, N = a.N, K = a.K;   // this workgroup's rows
   const uint8_t* const A = a.A + (int64_t)m0 * (uint32_t)a.lda;
   const float* const Sa = a.Sa + m0;
   uint16_t* const C = a.C + (int64_t)m0 * a.ldc;
@@ -65,13 +75,13 @@ __global__ __launch_bounds__(S8_NT, 2) void gemm_fp8_skinny_kernel(S8 a) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, q = lane >> 4;
-  const int bid = (int)blockIdx.x, c0 = bid * a.share + (bid < a.rest ? bid : a.rest), c1 = c0 + a.share + (bid < a.rest ? 1 : 0);
+  const int c0 = bid * a.share + (bid < a.rest ? bid : a.rest), c1 = c0 + a.share + (bid < a.rest ? 1 : 0);
   const int nblk = GB == 1 ? 1 : (c1 - c0 + CB - 1) / CB;
   // pieces p0 .. p1 - 1, of them first = p0 + wave, first + 8, ..., from `start` on and then from the first again
   int p0 = 0, p1 = (K + S8_KP - 1) / S8_KP;
   if (PARTS) {
     const int per = (p1 + (int)gridDim.y - 1) / (int)gridDim.y;
-    p0 = (int)blockIdx.y * per;
+    p0 = part_id * per;
     p1 = p0 + per < p1 ? p0 + per : p1;
   }
   const int first = p0 + wave, mine = p1 > first ? (p1 - first + S8_NW - 1) / S8_NW : 0;
@@ -242,7 +252,7 @@ __global__ __launch_bounds__(S8_NT, 2) void gemm_fp8_skinny_kernel(S8 a) {
         float sum = 0.f;
 #pragma unroll
         for (int w = 0; w < S8_NW; ++w) sum += reinterpret_cast<const float*>(smem)[w * (S8_RING / 4) + e];
-        if (PARTS) store_shared(part + (int64_t)blockIdx.y * part_size + (int64_t)gr * N + gc, sum);
+        if (PARTS) store_shared(part + part_id * part_size + (int64_t)gr * N + gc, sum);
         else C[(int64_t)gr * a.ldc + gc] = Elem<Tag>::from_f32(sum);
       }
     }
@@ -252,7 +262,7 @@ __global__ __launch_bounds__(S8_NT, 2) void gemm_fp8_skinny_kernel(S8 a) {
 
   // the last part of these columns to get here adds them all (EB elements of a thread at a time, all their parts requested
   // before the first is used: each such round is a trip to memory)
-  if (!last_to_arrive(a.counter + blockIdx.z * gridDim.x + bid, gridDim.y, reinterpret_cast<uint32_t*>(smem))) return;
+  if (!last_to_arrive(a.counter + bid * a.nz + z, gridDim.y, reinterpret_cast<uint32_t*>(smem))) return;
   const int cols = c1 - c0, parts = (int)gridDim.y;
   constexpr int EB = MT == 1 ? 2 : 4;
   for (int e0 = tid; e0 < M * cols; e0 += EB * S8_NT) {
@@ -297,9 +307,9 @@ int launch_s8_blocks(const GemmFp8Args& g, int rows, int parts, float* part, uns
     }
     configured_dev = dev;
   }
-  S8 a{(int)g.M, (int)g.N, (int)g.K, rows, (int)(g.N / nwg), (int)(g.N % nwg), (int)g.lda, (int)g.ldb, g.A, g.B, g.Sa, g.Sb, g.ldsa, g.ldsb, g.C, g.ldc, part,
+  S8 a{(int)g.M, (int)g.N, (int)g.K, rows, (int)(g.N / nwg), (int)(g.N % nwg), (int)g.lda, (int)g.ldb, (int)((g.M + rows - 1) / rows), device_xcds(), g.A, g.B, g.Sa, g.Sb, g.ldsa, g.ldsb, g.C, g.ldc, part,
        PARTS ? scratch_counters(part) : nullptr};
-  hipLaunchKernelGGL(kern, dim3(nwg, (unsigned)parts, (unsigned)((g.M + rows - 1) / rows)), dim3(S8_NT), S8_SMEM, s, a);
+  hipLaunchKernelGGL(kern, dim3(nwg * (unsigned)a.nz, (unsigned)parts), dim3(S8_NT), S8_SMEM, s, a);
   return hipGetLastError() == hipSuccess ? MLT_OK : MLT_ERR_LAUNCH;
 }
 

@@ -201,7 +201,7 @@ struct GemmFp8Args {
   int dtype;
   int forced = GEMM_AUTO, forced_parts = 0;   // as in GemmArgs; of the variants those that exist here: 256pp16, 128pp16, 256x128kp, 224x128kp, 192x128kp, 128kp, skinny
 };
-constexpr int64_t GEMM_FP8_FEW_ROWS = 1024;   // rows that gemm_fp8_skinny.hip takes, at most
+constexpr int64_t GEMM_FP8_FEW_ROWS = 4096;   // rows that gemm_fp8_skinny.hip takes, at most
 // rows of C of one of its workgroups: all of them up to 64, then equal shares of 16 n
 inline int gemm_fp8_skinny_rows(int64_t M) { const int64_t z = (M + 63) / 64; return (int)(M <= 64 ? M : (M + 16 * z - 1) / (16 * z) * 16); }
 int run_gemm_fp8_skinny(const GemmFp8Args& a, int parts, float* part, hipStream_t s);   // gemm_fp8_skinny.hip; parts 1 to 8; part: parts * M * N floats behind their counters

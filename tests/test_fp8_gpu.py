@@ -212,7 +212,7 @@ def test_gemm_k_split_across_workgroups(lib, k_parts, variant, parts, M, N, K):
 
 
 @pytest.mark.parametrize("parts", [1, 2, 8])
-@pytest.mark.parametrize("M", [65, 80, 129, 200, 333, 777, 1000, 1024])
+@pytest.mark.parametrize("M", [65, 80, 129, 200, 333, 777, 1000, 1024, 1500, 4096])
 def test_gemm_rows_shared_out(lib, k_parts, variant, parts, M):
     """More rows than one workgroup of the kernel for few rows takes: the last share ends inside a tile of 16 or before one; operands without a byte behind them."""
     k_parts(parts)
