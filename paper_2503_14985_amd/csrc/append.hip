@@ -26,7 +26,8 @@ namespace mlt {
 
 namespace {
 
-constexpr int AP_NT = 256;
+// threads of a workgroup whose units have W wavefronts: 4 units of one wavefront, or one unit
+constexpr int ap_threads(int W) { return W == 1 ? 256 : 64 * W; }
 
 // The largest b of [0, B) with start(b) <= i, or -1, by all 64 lanes together; start(b) does not fall with b.
 template <typename F>
@@ -113,10 +114,10 @@ __device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
   return u32x4{Elem<Tag>::pack2(x[0], x[1]), Elem<Tag>::pack2(x[2], x[3]), Elem<Tag>::pack2(x[4], x[5]), Elem<Tag>::pack2(x[6], x[7])};
 }
 
-template <typename Tag, int D, bool FP8, bool NEIGHBOURS>
+template <typename Tag, int D, bool FP8, bool NEIGHBOURS, int W>
 __device__ __forceinline__ void append_rows(const Append& a, int lane, int wave) {
   constexpr int LPR = D / 8, RPI = 64 / LPR;             // lanes per row, rows per access
-  const int w = (int)blockIdx.x * (AP_NT / 64) + wave;
+  const int w = (int)blockIdx.x * (ap_threads(W) / 64) + wave;
   const int t = w / a.parts, part = w % a.parts;
   if (t >= a.T) return;
   const int b = find_sequence([&](int j) { return a.offsets[j]; }, a.B, t, lane);
@@ -177,7 +178,7 @@ __device__ __forceinline__ void append_unit(const Append& a, int lane, int wave,
   constexpr int LPR = D / 8, RPI = 64 / LPR;
   constexpr int KEEP = 16 / RPI;                         // accesses whose rows stay in registers: 16 tokens
   const int upi = 2 * a.H;                               // units of an item
-  const int u = ((int)blockIdx.x - a.row_blocks) * (AP_NT / 64 / W) + (W == 1 ? wave : 0);
+  const int u = ((int)blockIdx.x - a.row_blocks) * (ap_threads(W) / 64 / W) + (W == 1 ? wave : 0);
   const int item = u / upi, hk = u % upi, sub = W == 1 ? 0 : wave;
   // item -> sequence and the block of it that new tokens fall in (touched blocks of b: at most its new tokens, and at most new / block_size + 2)
   const bool dense = a.dense_items != 0;
@@ -253,24 +254,45 @@ __device__ __forceinline__ void append_unit(const Append& a, int lane, int wave,
     float y[8];
     if (load(i0 + g, y)) store(i0 + g, y);
   }
-  if (slot0 > 0 && s != old) {                           // the earlier tokens of the block, in the new scale
+  if (slot0 > 0 && s != old) {                           // the earlier tokens of the block, in the new scale; eight accesses at once
     const float f = old * inv;
-    for (int i = sub * RPI + g; i < slot0; i += W * RPI) {
-      u32x2_mem* p = reinterpret_cast<u32x2_mem*>(dst + (int64_t)i * D + 8 * c);
-      const u32x2 v = *p;
-      const f32x4 lo = from_e4m3x4(v[0]), hi = from_e4m3x4(v[1]);
-      *p = u32x2{to_e4m3x4(lo[0] * f, lo[1] * f, lo[2] * f, lo[3] * f), to_e4m3x4(hi[0] * f, hi[1] * f, hi[2] * f, hi[3] * f)};
+    for (int i0 = sub * RPI + g; i0 < slot0; i0 += 8 * W * RPI) {
+      u32x2 v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + k * W * RPI < slot0 ? i0 + k * W * RPI : i0;
+        v[k] = *reinterpret_cast<const u32x2_mem*>(dst + (int64_t)i * D + 8 * c);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + k * W * RPI;
+        const f32x4 lo = from_e4m3x4(v[k][0]), hi = from_e4m3x4(v[k][1]);
+        if (i < slot0)
+          *reinterpret_cast<u32x2_mem*>(dst + (int64_t)i * D + 8 * c) =
+              u32x2{to_e4m3x4(lo[0] * f, lo[1] * f, lo[2] * f, lo[3] * f), to_e4m3x4(hi[0] * f, hi[1] * f, hi[2] * f, hi[3] * f)};
+      }
     }
   }
   if (sub == 0 && lane == 0 && s != old) *scale_at = s;
 }
 
 template <typename Tag, int D, bool FP8, bool NEIGHBOURS, int W>
-__global__ __launch_bounds__(AP_NT) void append_kernel(Append a) {
-  __shared__ float lds[AP_NT / 64];
+__global__ __launch_bounds__(ap_threads(W)) void append_kernel(Append a) {
+  __shared__ float lds[ap_threads(W) / 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (!FP8 || (int)blockIdx.x < a.row_blocks) append_rows<Tag, D, FP8, NEIGHBOURS>(a, lane, wave);
+  if (!FP8 || (int)blockIdx.x < a.row_blocks) append_rows<Tag, D, FP8, NEIGHBOURS, W>(a, lane, wave);
   else append_unit<Tag, D, NEIGHBOURS, W>(a, lane, wave, lds);
+}
+
+template <typename Tag, int D, bool FP8, bool NEIGHBOURS, int W>
+int launch_append_w(Append a, int64_t rows, int64_t units, hipStream_t s) {
+  constexpr int WAVES = ap_threads(W) / 64;
+  const int64_t row_blocks = rows ? ((int64_t)a.T * a.parts + WAVES - 1) / WAVES : 0, unit_blocks = (units * W + WAVES - 1) / WAVES;
+  if (row_blocks + unit_blocks > 0x7fffffff) return MLT_ERR_UNSUPPORTED;
+  if (row_blocks + unit_blocks == 0) return MLT_OK;
+  a.row_blocks = (int)row_blocks;
+  hipLaunchKernelGGL((append_kernel<Tag, D, FP8, NEIGHBOURS, W>), dim3((unsigned)(row_blocks + unit_blocks)), dim3(WAVES * 64), 0, s, a);
+  return hipGetLastError() == hipSuccess ? MLT_OK : MLT_ERR_LAUNCH;
 }
 
 template <typename Tag, int D, bool FP8, bool NEIGHBOURS>
@@ -281,23 +303,18 @@ int launch_append(const AppendArgs& g, hipStream_t s) {
   const int64_t rows = FP8 ? g.Hq : g.Hq + 2 * g.H;
   // a token's rows over several wavefronts where there are few tokens
   while (a.parts < 16 && g.T * a.parts < 2048 && rows > RPI * a.parts) a.parts *= 2;
-  const int64_t row_blocks = rows ? (g.T * a.parts + AP_NT / 64 - 1) / (AP_NT / 64) : 0;
-  int64_t unit_blocks = 0;
-  bool wide = false;
-  if (FP8) {
-    const int64_t by_block = g.T / g.block_size + 2 * g.B;
-    a.dense_items = g.T <= by_block;
-    const int64_t units = (a.dense_items ? g.T : by_block) * 2 * g.H;
-    // Four wavefronts to a unit where a unit has more than 32 new tokens for the most part, not for single tokens (255 tokens, 16 heads: 10.8 us, with four 28.3)
-    wide = !a.dense_items && g.block_size > 32;
-    unit_blocks = wide ? units : (units + AP_NT / 64 - 1) / (AP_NT / 64);
-  }
-  if (row_blocks + unit_blocks > 0x7fffffff) return MLT_ERR_UNSUPPORTED;
-  if (row_blocks + unit_blocks == 0) return MLT_OK;
-  a.row_blocks = (int)row_blocks;
-  auto kern = wide ? append_kernel<Tag, D, FP8, NEIGHBOURS, FP8 ? 4 : 1> : append_kernel<Tag, D, FP8, NEIGHBOURS, 1>;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(row_blocks + unit_blocks)), dim3(AP_NT), 0, s, a);
-  return hipGetLastError() == hipSuccess ? MLT_OK : MLT_ERR_LAUNCH;
+  if (!FP8) return launch_append_w<Tag, D, FP8, NEIGHBOURS, 1>(a, rows, 0, s);
+  const int64_t by_block = g.T / g.block_size + 2 * g.B;
+  a.dense_items = g.T <= by_block;
+  const int64_t units = (a.dense_items ? g.T : by_block) * 2 * g.H;
+  // As many wavefronts to a unit as hold its new tokens in registers, 16 each (8191 tokens, 8 heads of 128, blocks of 32, 64, 128: 37.2, 37.5, 39.9 us; with four
+  // wavefronts 42.2, 37.5, 45.2; with one 43.7, 51.2, 72.8); one for single tokens, whatever the block size (255 tokens, 16 heads: 10.8 us, with four 28.3)
+  const int64_t w = a.dense_items ? 1 : g.block_size / 16;
+  if (w <= 1) return launch_append_w<Tag, D, true, NEIGHBOURS, 1>(a, rows, units, s);
+  if (w <= 2) return launch_append_w<Tag, D, true, NEIGHBOURS, 2>(a, rows, units, s);
+  if (w <= 4) return launch_append_w<Tag, D, true, NEIGHBOURS, 4>(a, rows, units, s);
+  if (w <= 8) return launch_append_w<Tag, D, true, NEIGHBOURS, 8>(a, rows, units, s);
+  return launch_append_w<Tag, D, true, NEIGHBOURS, 16>(a, rows, units, s);
 }
 
 template <typename Tag, int D>
