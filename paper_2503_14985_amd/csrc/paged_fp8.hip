@@ -472,13 +472,14 @@ int run_paged_fp8_t(const PagedFp8Args& a, bool wide, int tiles, int nsplit, flo
 
 // Key ranges per (sequence, head): up to two workgroups of 8 wavefronts on every CU, which is what a CU holds (48 sequences of 2048 keys and 8 heads: 24.4 us
 // with one range, 27.9 with two, which make 768), with 8 units a range or more (one to a
-// wavefront). A single sequence has no long and short pieces to even out and gets one workgroup a CU: one of 32768 keys and 8 heads 17.0 us with 32 ranges, 18.2
+// wavefront; ranges are whole multiples of that: 2000 keys in 8 ranges 7.9 us, in 7 9.1). A single sequence has no long and short pieces to even out and gets one workgroup a CU: one of 32768 keys and 8 heads 17.0 us with 32 ranges, 18.2
 // with 64. 9 to 16 ranges need the second kernel and do not repay it: 4 sequences of 4096 keys 10.1 us with 8, 12.5 with 16 (of 32768: 35.5 and 34.2).
 int plan_paged_fp8_split(const PagedFp8Args& a, int64_t wgs, int64_t ncu) {
   if (a.forced_split > 0) return a.forced_split > PF_MAX_SPLIT ? PF_MAX_SPLIT : a.forced_split;
   const int64_t units = (a.max_blocks * a.block_size + PF_UNIT - 1) / PF_UNIT;
   int64_t n = (a.B > 1 ? 2 : 1) * ncu / wgs;
-  if (n > units / 8) n = units / 8;
+  if (n > (units + 7) / 8) n = (units + 7) / 8;
+  if (units <= 16) n = 1;                                // (two sequences of 300 keys: 4.8 us, in 2 ranges 6.0)
   if (n > PF_LAST_SPLIT && n <= 2 * PF_LAST_SPLIT) n = PF_LAST_SPLIT;
   if (n > PF_MAX_SPLIT) n = PF_MAX_SPLIT;
   return n < 1 ? 1 : (int)n;
