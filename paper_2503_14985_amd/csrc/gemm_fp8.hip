@@ -569,7 +569,7 @@ Fp8Plan plan_fp8(const GemmFp8Args& a, int max_parts, int64_t ncu) {
   for (int parts = 1; parts <= max_parts; parts *= 2) {
     if (a.forced_parts > 0 ? parts != a.forced_parts && max_parts > 1 : parts > 1 && (parts * a.M * a.N * 4 > kStaticScratchBytes || a.K < 256 * parts)) continue;
     for (int v : tall) offer(v, parts);
-    if (a.M <= GEMM_FP8_FEW_ROWS && parts <= 8) offer(GEMM_SKINNY, parts);
+    if (a.M <= GEMM_FP8_FEW_ROWS) offer(GEMM_SKINNY, parts);
   }
   if (a.forced_parts <= 1 || max_parts == 1 || best.parts == 1) {
     offer(GEMM_256_PP16, 1);
@@ -587,7 +587,7 @@ int run_fp8_t(const GemmFp8Args& a, hipStream_t s, char* name, size_t size) {
   }
   DeviceInfo di;
   const int64_t ncu = device_info(di) && di.ncu > 0 ? di.ncu : 256;
-  Fp8Plan p = plan_fp8(a, 16, ncu);
+  Fp8Plan p = plan_fp8(a, 8, ncu);
   float* part = nullptr;
   if (p.parts > 1) {
     part = cached_scratch(p.parts * a.M * a.N * (int64_t)sizeof(float), s);

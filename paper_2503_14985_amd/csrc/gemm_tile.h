@@ -471,8 +471,7 @@ template <typename Tag>
 static int launch_splitk_reduce(const GemmArgs& g, int parts, int64_t part_stride, hipStream_t s) {
   const int64_t nthreads = g.M * ((g.N + 3) / 4);
   auto kern = parts <= 2 ? gemm_splitk_reduce_kernel<Tag, 2> : parts <= 4 ? gemm_splitk_reduce_kernel<Tag, 4>
-                                                             : parts <= 8 ? gemm_splitk_reduce_kernel<Tag, 8>
-                                                                          : gemm_splitk_reduce_kernel<Tag, 16>;
+                                                                          : gemm_splitk_reduce_kernel<Tag, 8>;
   hipLaunchKernelGGL(kern, dim3((unsigned)((nthreads + 255) / 256)), dim3(256), 0, s, (int)g.M, (int)g.N,
                      parts, g.scratch, part_stride, g.C, g.ldc, g.epi(), g.bias);
   return hipGetLastError() == hipSuccess ? MLT_OK : MLT_ERR_LAUNCH;

@@ -151,7 +151,7 @@ int append_call(const AppendArgs& a, bool fp8, void* stream) {
   if (a.D != 64 && a.D != 128) return MLT_ERR_UNSUPPORTED;
   if (a.block_size % 16 || a.block_size > 1024 || a.rot % 16) return MLT_ERR_UNSUPPORTED;
   if (a.T == 0 || a.B == 0 || a.Hq + a.H == 0) return MLT_OK;
-  if (a.T > INT_MAX || a.B > INT_MAX / 4 || a.Hq > INT_MAX / 4 / a.D || a.H > INT_MAX / 4 / a.D || a.num_blocks > INT_MAX || a.max_blocks > INT_MAX ||
+  if (a.T > INT_MAX - 64 || a.B > INT_MAX / 4 || a.Hq > INT_MAX / 4 / a.D || a.H > INT_MAX / 4 / a.D || a.num_blocks > INT_MAX || a.max_blocks > INT_MAX ||
       a.max_blocks * a.block_size > INT_MAX || a.positions > INT_MAX) return MLT_ERR_UNSUPPORTED;
   if (!a.offsets || !a.seq_lens || !a.block_table || !aligned(a.offsets, 4) || !aligned(a.seq_lens, 4) || !aligned(a.block_table, 4)) return MLT_ERR_INVALID_ARG;
   if (a.rot && (!a.cos || !a.sin || !aligned(a.cos, 4) || !aligned(a.sin, 4) || a.positions < 1)) return MLT_ERR_INVALID_ARG;
@@ -432,7 +432,7 @@ int mlt_paged_attn_decode_fp8(int64_t B, int64_t Hq, int64_t H, int64_t D, int64
   if (!Q || !Kc || !Vc || !Ks || !Vs || !block_table || !seq_lens || !O) return MLT_ERR_INVALID_ARG;
   if (!aligned(Q, 16) || !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(O, 2) || !aligned(Ks, 4) || !aligned(Vs, 4) || !aligned(block_table, 4) ||
       !aligned(seq_lens, 4)) return MLT_ERR_INVALID_ARG;
-  if (B > INT_MAX || Hq > INT_MAX || B * Hq > INT_MAX || max_blocks > INT_MAX || max_blocks * block_size > INT_MAX || num_blocks > INT_MAX) return MLT_ERR_UNSUPPORTED;
+  if (B > INT_MAX || Hq > INT_MAX || B * Hq > INT_MAX || max_blocks > INT_MAX || max_blocks * block_size > INT_MAX - 1024 || num_blocks > INT_MAX) return MLT_ERR_UNSUPPORTED;
   if (num_blocks * H > INT_MAX || num_blocks * H * (block_size / 16) > INT_MAX) return MLT_ERR_UNSUPPORTED;   // units of 16 rows are counted in 32 bits
   if (!device_is_gfx950()) return MLT_ERR_DEVICE;
   PagedFp8Args a{B, Hq, H, D, block_size, max_blocks, num_blocks, (const uint16_t*)Q, (const uint8_t*)Kc, (const uint8_t*)Vc, Ks, Vs, block_table,

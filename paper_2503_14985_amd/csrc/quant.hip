@@ -56,10 +56,11 @@ __device__ __forceinline__ u32x2 quant8(const u32x4& v, float inv) {
 // A workgroup takes 4 * RPW rows and 4 blocks of columns, a wavefront RPW rows of them.
 template <typename Tag, int RPW>
 __global__ __launch_bounds__(QT_NT) void quant_rows_kernel(int M, int K, const uint16_t* __restrict__ X, int64_t ldx,
-                                                           uint8_t* __restrict__ Xq, int64_t ldq, float* __restrict__ S, int64_t lds) {
+                                                           uint8_t* __restrict__ Xq, int64_t ldq, float* __restrict__ S, int64_t lds, int nbx) {
   __shared__ float sc[4][4 * RPW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int row0 = (int)blockIdx.y * 4 * RPW, col = (int)blockIdx.x * 512 + lane * 8;
+  const int by = (int)blockIdx.x / nbx, bx = (int)blockIdx.x - by * nbx;
+  const int row0 = by * 4 * RPW, col = bx * 512 + lane * 8;
   const bool in = col < K;
   u32x4 v[RPW];
   const uint16_t* x = X + (in ? col : K - 8);
@@ -77,7 +78,7 @@ __global__ __launch_bounds__(QT_NT) void quant_rows_kernel(int M, int K, const u
   }
   __syncthreads();
   for (int e = tid; e < 16 * RPW; e += QT_NT) {
-    const int kb = (int)blockIdx.x * 4 + e / (4 * RPW), r = row0 + e % (4 * RPW);
+    const int kb = bx * 4 + e / (4 * RPW), r = row0 + e % (4 * RPW);
     if (r < M && kb * F8_KB < K) S[(int64_t)kb * lds + r] = sc[e / (4 * RPW)][e % (4 * RPW)];
   }
 }
@@ -85,10 +86,11 @@ __global__ __launch_bounds__(QT_NT) void quant_rows_kernel(int M, int K, const u
 // A workgroup takes a block of 128 x 128, a wavefront 32 rows of it.
 template <typename Tag>
 __global__ __launch_bounds__(QT_NT) void quant_tiles_kernel(int M, int K, const uint16_t* __restrict__ X, int64_t ldx,
-                                                            uint8_t* __restrict__ Xq, int64_t ldq, float* __restrict__ S, int64_t lds) {
+                                                            uint8_t* __restrict__ Xq, int64_t ldq, float* __restrict__ S, int64_t lds, int nbx) {
   __shared__ float top[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int row0 = (int)blockIdx.y * 128 + wave * 32 + (lane >> 4), col = (int)blockIdx.x * F8_KB + (lane & 15) * 8;
+  const int by = (int)blockIdx.x / nbx, bx = (int)blockIdx.x - by * nbx;
+  const int row0 = by * 128 + wave * 32 + (lane >> 4), col = bx * F8_KB + (lane & 15) * 8;
   const bool in = col < K;
   u32x4 v[8];
   const uint16_t* x = X + (in ? col : K - 8);
@@ -109,19 +111,18 @@ __global__ __launch_bounds__(QT_NT) void quant_tiles_kernel(int M, int K, const 
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (in && row0 + 4 * i < M) *reinterpret_cast<u32x2_mem*>(Xq + (int64_t)(row0 + 4 * i) * ldq + col) = quant8<Tag>(v[i], inv);
-  if (tid == 0) S[(int64_t)blockIdx.x * lds + blockIdx.y] = s;
+  if (tid == 0) S[(int64_t)bx * lds + by] = s;
 }
 
 template <typename Tag>
 int run_quant_t(const QuantArgs& a, hipStream_t s) {
-  const unsigned kb = (unsigned)((a.K + F8_KB - 1) / F8_KB);
-  if (a.block_rows == 1) {
-    constexpr int RPW = 4;
-    hipLaunchKernelGGL((quant_rows_kernel<Tag, RPW>), dim3((kb + 3) / 4, (unsigned)((a.M + 4 * RPW - 1) / (4 * RPW))), dim3(QT_NT), 0, s, (int)a.M, (int)a.K,
-                       a.X, a.ldx, a.Xq, a.ldq, a.S, a.lds);
-  } else {
-    hipLaunchKernelGGL((quant_tiles_kernel<Tag>), dim3(kb, (unsigned)((a.M + 127) / 128)), dim3(QT_NT), 0, s, (int)a.M, (int)a.K, a.X, a.ldx, a.Xq, a.ldq, a.S, a.lds);
-  }
+  constexpr int RPW = 4;
+  const int64_t cols = a.block_rows == 1 ? 512 : F8_KB, rows = a.block_rows == 1 ? 4 * RPW : 128, nbx = (a.K + cols - 1) / cols, wgs = nbx * ((a.M + rows - 1) / rows);
+  if (wgs > 0x7fffffff) return MLT_ERR_UNSUPPORTED;
+  if (a.block_rows == 1)
+    hipLaunchKernelGGL((quant_rows_kernel<Tag, RPW>), dim3((unsigned)wgs), dim3(QT_NT), 0, s, (int)a.M, (int)a.K, a.X, a.ldx, a.Xq, a.ldq, a.S, a.lds, (int)nbx);
+  else
+    hipLaunchKernelGGL((quant_tiles_kernel<Tag>), dim3((unsigned)wgs), dim3(QT_NT), 0, s, (int)a.M, (int)a.K, a.X, a.ldx, a.Xq, a.ldq, a.S, a.lds, (int)nbx);
   return hipGetLastError() == hipSuccess ? MLT_OK : MLT_ERR_LAUNCH;
 }
 

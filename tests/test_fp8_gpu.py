@@ -95,6 +95,15 @@ def gemm_operands(M, N, K, seed):
     return a, sa, b, sb
 
 
+@pytest.mark.parametrize("rows,M,K", [(1, 1200000, 16), (128, 8500000, 8)])
+def test_quant_many_rows(lib, rows, M, K):
+    """More rows than a launch has in its second dimension. Small whole numbers times a power of two per row (per 128 rows): they come back exactly."""
+    r = torch.arange(M, device=dev(), dtype=torch.int32)
+    x = ((r[:, None] + torch.arange(K, device=dev(), dtype=torch.int32)) % 7 - 3).to(BF16) * torch.exp2((r // rows % 5).float()).to(BF16)[:, None]
+    q, s = lib.mlt_quant_fp8(x, rows)
+    assert torch.equal(q.to(BF16) * s[0].repeat_interleave(rows)[:M, None].to(BF16), x)
+
+
 def gemm_check(C, a, sa, b, sb, dtype, K):
     ref, mass, top = u.gemm(f64(a), f64(sa), f64(b), f64(sb))
     tol = u.gemm_tolerance(ref, mass, top, K, sa.shape[0], dtype)
