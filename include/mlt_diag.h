@@ -78,7 +78,7 @@ int mlt_query_tiling(int op, const int64_t dims[4], int dtype, int32_t out[10]);
  * problem (alignment, shape) falls back to one that can, as the automatic choice would.
  *   gemm_variant  "general", "256", "256w8", "256pp16", "128pp16", "128pp16k128", "256x128kp", "224x128kp", "192x128kp", "160x128kp", "128kp", "256w4", "256w8x1",
  *                 "256w1x8", "128w8", "64x128", "64", "128k2", "64x128k2", "64k4", "skinny" (or its older name "skinnydma")
- *                 mlt_gemm_fp8 has those of the names 256pp16, 128pp16, 256x128kp, 224x128kp, 192x128kp, 128kp and skinny, and its own choice for the others.
+ *                 mlt_gemm_fp8 has those of the names 256pp16, 128pp16, 256x128kp, 224x128kp, 192x128kp, 128kp and skinny (up to 4096 rows), and its own choice for the others.
  *   mha_variant   "pp32", "pp16", "ps", "k2", "k4"
  * The initial values come from the environment variables MLT_GEMM_VARIANT and MLT_MHA_VARIANT,
  * which are read once, at the first call that needs them. Not synchronised with compute calls
