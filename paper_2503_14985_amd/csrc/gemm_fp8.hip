@@ -14,7 +14,7 @@
 // all earlier ones: A of the next step has to have landed by the end of that phase anyway, and B has.
 //
 // The 128-column tiles (gemm_fp8_kp_kernel) follow gemm_kp.hip: 256 to 128 rows x 128 columns, the two groups on alternate K steps, the scales in the LDS stage of their
-// step; K may be split in up to 8 parts, added by gemm_splitk_reduce_kernel. Which kernel runs is decided by estimated time (fp8_estimate).
+// step; K may be split in two parts, joined by the workgroup that comes last, or in up to 8, added by gemm_splitk_reduce_kernel. Which kernel runs is decided by estimated time (fp8_estimate).
 //
 // Measured: 8192 x 8192 x 8192 423 us, 2600 TFLOP/s (219 us of the matrix units' time at 2.4 GHz; the board's power holds the clock below that); 777 x 4096 x 14336 61 us by 224 x 128 tiles
 // and two parts, 1490 TFLOP/s (bound by delivery: a CU takes 45 KB a step). A K step of a 256 x 256 tile, 1.98 us on random bits (1.65 on quantised N(0, 1)):
@@ -287,6 +287,8 @@ template <int BM> struct K8Tile {
   static constexpr int NL = NLA + NLB + 1;                               // and one of scales
   static constexpr int S = 128 + 4;                                      // floats per row of a group's image of the result
   static constexpr int RPP = BM / 2;                                     // rows per pass of the epilogue
+  static constexpr int EP = (RPP * 16 + G8_NT - 1) / G8_NT;              // pieces of 8 columns per thread and pass
+  static constexpr int PART = 2 * EP * 8 * G8_NT;                        // floats of a part of a tile
   static constexpr int IMG_B = 2 * RPP * S * 4;
   static constexpr int SMEM = R * STAGE > IMG_B ? R * STAGE : IMG_B;
 };
@@ -296,7 +298,7 @@ template <int BM> struct K8Tile {
 template <typename Tag, int BM, bool TAIL>
 __global__ __launch_bounds__(G8_NT, 2) void gemm_fp8_kp_kernel(int M, int N, int K_, const uint8_t* __restrict__ A, int64_t lda, const float* __restrict__ Sa, int64_t ldsa,
                                                                const uint8_t* __restrict__ B, int64_t ldb, const float* __restrict__ Sb, int64_t ldsb, uint16_t* __restrict__ C,
-                                                               int64_t ldc, int nbm, int nbn, int nxcd, int part_steps, float* __restrict__ part_out) {
+                                                               int64_t ldc, int nbm, int nbn, int nxcd, int part_steps, int joined, float* part_out) {
   typedef K8Tile<BM> T;
   constexpr int R = T::R, NL = T::NL, NLA = T::NLA, NLB = T::NLB, WTM = BM / 2, WTN = 64, TA = WTM / 16, TB = WTN / 16;
   extern __shared__ __align__(16) char smem[];
@@ -320,6 +322,7 @@ __global__ __launch_bounds__(G8_NT, 2) void gemm_fp8_kp_kernel(int M, int N, int
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int grp = wave >> 2, w = wave & 3, wm = w >> 1, wn = w & 1;
+  const int tile = logical;
   int tile_m, tile_n;
   tile_of_logical<G8_GROUP_M>(logical, nbm, nbn, tile_m, tile_n);
   const int m0 = tile_m * BM, n0 = tile_n * 128;
@@ -425,9 +428,11 @@ __global__ __launch_bounds__(G8_NT, 2) void gemm_fp8_kp_kernel(int M, int N, int
   }
   if ((KT & 1) == grp) MLT_BARRIER();                     // KT + 1 phases for both groups
 
-  // ---- epilogue: RPP rows at a time both groups park their accumulators in images of their own; all threads add the two
+  // ---- epilogue: RPP rows at a time both groups park their accumulators in images of their own; all threads add the two, 8 columns a piece
   float* const img = reinterpret_cast<float*>(smem);
-  constexpr int S = T::S, RPP = T::RPP;
+  constexpr int S = T::S, RPP = T::RPP, EP = T::EP;
+  const bool in_rows = part_steps > 0 && !joined;        // a part's sums as rows, for another kernel to add up
+  f32x4 sum[BM / RPP][EP][2];
 #pragma unroll
   for (int p = 0; p < BM / RPP; ++p) {
     if (p > 0) __syncthreads();
@@ -439,25 +444,60 @@ __global__ __launch_bounds__(G8_NT, 2) void gemm_fp8_kp_kernel(int M, int N, int
         for (int j = 0; j < TB; ++j) *reinterpret_cast<f32x4_mem*>(mine + i * 16 * S + j * 16) = acc[i][j];
     }
     __syncthreads();
-    const int row0 = m0 + p * RPP;
-    if (part_steps > 0) {
+    if (in_rows) {
       for (int e = tid; e < RPP * 32; e += G8_NT) {
-        const int r = e / 32, c = e % 32 * 4;
+        const int r = e / 32, c = e % 32 * 4, row = m0 + p * RPP + r;
         f32x4 v = *reinterpret_cast<const f32x4_mem*>(img + r * S + c);
         add4(v, *reinterpret_cast<const f32x4_mem*>(img + (RPP + r) * S + c));
-        if (row0 + r < M && n0 + c < N) store_row4(v, part_out + ((int64_t)part * M + row0 + r) * N + n0 + c, N - n0 - c, false);
+        if (row < M && n0 + c < N) store_row4(v, part_out + ((int64_t)part * M + row) * N + n0 + c, N - n0 - c, false);
       }
-    } else {
-      for (int e = tid; e < RPP * 16; e += G8_NT) {
-        const int r = e / 16, c = e % 16 * 8;
-        const float* src = img + r * S + c;
-        f32x4 lo = *reinterpret_cast<const f32x4_mem*>(src), hi = *reinterpret_cast<const f32x4_mem*>(src + 4);
-        add4(lo, *reinterpret_cast<const f32x4_mem*>(src + RPP * S));
-        add4(hi, *reinterpret_cast<const f32x4_mem*>(src + RPP * S + 4));
-        if (row0 + r < M && n0 + c < N) store_row8<Tag, false>(lo, hi, C + (int64_t)(row0 + r) * ldc + n0 + c, N - n0 - c, 0, nullptr);
+      continue;
+    }
+#pragma unroll
+    for (int i = 0; i < EP; ++i) {
+      const int e = i * G8_NT + tid < RPP * 16 ? i * G8_NT + tid : 0;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float* src = img + e / 16 * S + e % 16 * 8 + 4 * k;
+        sum[p][i][k] = *reinterpret_cast<const f32x4_mem*>(src);
+        add4(sum[p][i][k], *reinterpret_cast<const f32x4_mem*>(src + RPP * S));
       }
     }
   }
+  if (in_rows) return;
+  if (joined) {
+    // two parts: both leave their sums, a thread's next to those of its neighbours, and the one of a tile that comes last adds the other's (a sum of two has no order)
+    auto place = [&](int q) __attribute__((always_inline)) { return part_out + (int64_t)(q * tiles + tile) * T::PART + tid; };
+    float* mine = place(part);
+#pragma unroll
+    for (int p = 0; p < BM / RPP; ++p)
+#pragma unroll
+      for (int i = 0; i < EP; ++i)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) store_shared(mine + ((p * EP + i) * 8 + c) * G8_NT, sum[p][i][c / 4][c % 4]);
+    if (!last_to_arrive(reinterpret_cast<uint32_t*>(part_out) - kScratchCounters + tile, 2u, reinterpret_cast<uint32_t*>(smem))) return;
+    const float* other = place(1 - part);
+    float v[BM / RPP][EP][8];
+#pragma unroll
+    for (int p = 0; p < BM / RPP; ++p)
+#pragma unroll
+      for (int i = 0; i < EP; ++i)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[p][i][c] = load_shared(other + ((p * EP + i) * 8 + c) * G8_NT);
+#pragma unroll
+    for (int p = 0; p < BM / RPP; ++p)
+#pragma unroll
+      for (int i = 0; i < EP; ++i)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) sum[p][i][c / 4][c % 4] += v[p][i][c];
+  }
+#pragma unroll
+  for (int p = 0; p < BM / RPP; ++p)
+#pragma unroll
+    for (int i = 0; i < EP; ++i) {
+      const int e = i * G8_NT + tid, r = m0 + p * RPP + e / 16, c = n0 + e % 16 * 8;
+      if (e < RPP * 16 && r < M && c < N) store_row8<Tag, false>(sum[p][i][0], sum[p][i][1], C + (int64_t)r * ldc + c, N - c, 0, nullptr);
+    }
 }
 
 namespace {
@@ -505,11 +545,12 @@ int launch_fp8_kp(const GemmFp8Args& a, int parts, float* part, hipStream_t s) {
   const int64_t nbm = (a.M + BM - 1) / BM, nbn = (a.N + 127) / 128;
   if (nbm * nbn * parts > 0x7fffffff) return MLT_ERR_UNSUPPORTED;
   const int KT = (int)((a.K + F8_KB - 1) / F8_KB), part_steps = parts > 1 ? (KT + parts - 1) / parts : 0;
+  const bool joined = parts == 2 && part_steps < KT;     // (as part_bytes has it)
   if (parts > 1) parts = (KT + part_steps - 1) / part_steps;                // no empty part
   hipLaunchKernelGGL(kern, dim3((unsigned)(nbm * nbn * parts)), dim3(G8_NT), SMEM, s, (int)a.M, (int)a.N, (int)a.K, a.A, a.lda, a.Sa, a.ldsa, a.B, a.ldb, a.Sb, a.ldsb, a.C,
-                     a.ldc, (int)nbm, (int)nbn, device_xcds(), part_steps, part);
+                     a.ldc, (int)nbm, (int)nbn, device_xcds(), part_steps, joined ? 1 : 0, part);
   if (hipGetLastError() != hipSuccess) return MLT_ERR_LAUNCH;
-  if (part_steps == 0) return MLT_OK;
+  if (part_steps == 0 || joined) return MLT_OK;
   GemmArgs g{a.M, a.N, a.K, nullptr, 0, nullptr, 0, 1, a.C, a.ldc, a.dtype, GEMM_AUTO, 0};
   g.scratch = part;
   return run_splitk_reduce(g, parts, a.M * a.N, s);
@@ -557,10 +598,20 @@ double fp8_estimate(int variant, int parts, int64_t M, int64_t N, int64_t K, int
                : variant == GEMM_224X128_KP ? Cost{224, 128, 0.75, 0.09, 3.2, 3.7}
                : variant == GEMM_192X128_KP ? Cost{192, 128, 0.69, 0.07, 3.0, 3.6} : Cost{128, 128, 0.56, 0.06, 2.6, 3.3};
   const int64_t w = tiles(c.bm, c.bn), rounds = (w + ncu - 1) / ncu;
-  return c.launch + steps * (c.step * rounds + c.fill * w / ncu) + c.round * rounds + 0.3 * mb + (parts > 1 ? 2.5 + parts * (0.2 + 1.4 * mb) : 0.0);
+  return c.launch + steps * (c.step * rounds + c.fill * w / ncu) + c.round * rounds + 0.3 * mb + (parts == 2 ? 3.2 + 1.65 * mb : parts > 2 ? 2.5 + parts * (0.2 + 1.4 * mb) : 0.0);
 }
 
 struct Fp8Plan { int variant, parts; };
+
+int64_t kp_rows_of(int variant) { return variant == GEMM_256X128_KP ? 256 : variant == GEMM_224X128_KP ? 224 : variant == GEMM_192X128_KP ? 192 : 128; }
+int64_t kp_tiles(int variant, const GemmFp8Args& a) { return (a.M + kp_rows_of(variant) - 1) / kp_rows_of(variant) * ((a.N + 127) / 128); }
+// Bytes of the partial results of a plan with K in parts. Two parts of a tile are joined by the workgroup that comes last (777 x 4096 x 14336: 61.4 us, by a second kernel
+// 65.1; 512 x 4096 x 4096 22.8 and 24.1), more by a second kernel (400 x 4096 x 8192 in four 30.5 us, joined 36.0).
+int64_t part_bytes(const Fp8Plan& p, const GemmFp8Args& a) {
+  if (p.variant == GEMM_SKINNY || p.parts > 2) return p.parts * a.M * a.N * (int64_t)sizeof(float);
+  const int64_t floats = p.variant == GEMM_256X128_KP ? K8Tile<256>::PART : p.variant == GEMM_224X128_KP ? K8Tile<224>::PART : p.variant == GEMM_192X128_KP ? K8Tile<192>::PART : K8Tile<128>::PART;
+  return p.parts * kp_tiles(p.variant, a) * floats * (int64_t)sizeof(float);
+}
 
 Fp8Plan plan_fp8(const GemmFp8Args& a, int max_parts, int64_t ncu) {
   static const int tall[] = {GEMM_256X128_KP, GEMM_224X128_KP, GEMM_192X128_KP, GEMM_128_KP};
@@ -570,11 +621,13 @@ Fp8Plan plan_fp8(const GemmFp8Args& a, int max_parts, int64_t ncu) {
   double least = 1e30;
   auto offer = [&](int v, int parts) {
     if (forced != GEMM_AUTO && v != forced) return;
+    if (parts == 2 && v != GEMM_SKINNY && kp_tiles(v, a) > kScratchCounters) return;       // a counter for each tile
+    if (parts > 1 && a.forced_parts == 0 && part_bytes(Fp8Plan{v, parts}, a) > kStaticScratchBytes) return;
     const double t = fp8_estimate(v, parts, a.M, a.N, a.K, ncu);
     if (t < least) { least = t; best = Fp8Plan{v, parts}; }
   };
   for (int parts = 1; parts <= max_parts; parts *= 2) {
-    if (a.forced_parts > 0 ? parts != a.forced_parts && max_parts > 1 : parts > 1 && (parts * a.M * a.N * 4 > kStaticScratchBytes || a.K < 256 * parts)) continue;
+    if (a.forced_parts > 0 ? parts != a.forced_parts && max_parts > 1 : parts > 1 && a.K < 256 * parts) continue;
     for (int v : tall) offer(v, parts);
     if (a.M <= GEMM_FP8_FEW_ROWS) offer(GEMM_SKINNY, parts);
   }
@@ -597,7 +650,7 @@ int run_fp8_t(const GemmFp8Args& a, hipStream_t s, char* name, size_t size) {
   Fp8Plan p = plan_fp8(a, 8, ncu);
   float* part = nullptr;
   if (p.parts > 1) {
-    part = cached_scratch(p.parts * a.M * a.N * (int64_t)sizeof(float), s);
+    part = cached_scratch(part_bytes(p, a), s);
     if (!part) p = plan_fp8(a, 1, ncu);                  // no scratch to be had: the best of the plain forms
   }
   const char* tile = p.variant == GEMM_SKINNY ? "skinny" : p.variant == GEMM_256_PP16 ? "256x256_pp" : p.variant == GEMM_128_PP16 ? "128x128_pp" : p.variant == GEMM_256X128_KP ? "256x128_kp"
