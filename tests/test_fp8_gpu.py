@@ -663,6 +663,64 @@ def test_on_another_stream(lib):
         assert torch.equal(y, want)
 
 
+def test_split_calls_on_two_streams_at_once(lib):
+    """Calls that spread one result over workgroups, on two streams that overlap: each stream has its own partial results and counters."""
+    def product(M, N, K, seed):
+        at = [t.to(dev()) for t in gemm_operands(M, N, K, seed)]
+        return lambda stream: lib.mlt_gemm_fp8(*at, stream=stream)
+
+    def attention(B, H, n, seed):
+        g = torch.Generator(device=dev())
+        g.manual_seed(seed)
+        per = -(-n // 16)
+        kc, vc = (torch.randn((B * per, H, 16, 128), generator=g, device=dev()).to(F8) for _ in range(2))
+        ks, vs = (torch.rand((B * per, H), generator=g, device=dev()) + 0.1 for _ in range(2))
+        table = torch.randperm(B * per, generator=g, device=dev()).to(torch.int32).reshape(B, per).contiguous()
+        q = torch.randn((B, 2 * H, 128), generator=g, device=dev()).to(BF16)
+        lens = torch.full((B,), n, dtype=torch.int32, device=dev())
+        return lambda stream: lib.mlt_paged_attn_decode_fp8(q, kc, vc, ks, vs, table, lens, 0.1, stream=stream)
+
+    calls = [product(512, 4096, 2048, 1), product(64, 512, 8192, 2), attention(4, 2, 3000, 3), attention(1, 2, 9000, 4), product(130, 2048, 8192, 5), attention(2, 8, 2100, 6)]
+    want, names = [], []
+    for c in calls:
+        want.append(c(None).clone())
+        names.append(lib.mlt_last_kernel())
+    assert sum("split" in n for n in names) >= 4, names
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(4):
+        got = [[c(s) for c in (calls if s is sides[0] else calls[::-1])] for s in sides]
+        torch.cuda.synchronize()
+        for a, b, w in zip(got[0], got[1][::-1], want):
+            assert torch.equal(a, w) and torch.equal(b, w)
+
+
+def test_captured_calls_that_would_split(lib):
+    """Captured, nothing is spread over workgroups through scratch: replays between eager calls that are give the same bits each time, and those of the eager
+    calls up to the order of the sums."""
+    at = [t.to(dev()) for t in gemm_operands(512, 4096, 2048, 11)]
+    eager = lib.mlt_gemm_fp8(*at)
+    C = torch.empty_like(eager)
+    graph, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lib.mlt_gemm_fp8(*at, C=C)
+    C2 = torch.empty_like(eager)
+    with torch.cuda.graph(other):
+        lib.mlt_gemm_fp8(*at, C=C2)
+    first = None
+    for _ in range(5):
+        graph.replay()
+        again = lib.mlt_gemm_fp8(*at)
+        other.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(again, eager) and torch.equal(C, C2)
+        first = C.clone() if first is None else first
+        assert torch.equal(C, first)
+        C.zero_()
+        C2.zero_()
+    gemm_check(first[:64], at[0][:64].cpu(), at[1][:, :64].cpu(), at[2].cpu(), at[3].cpu(), BF16, 2048)
+
+
 def test_captured_and_replayed(lib):
     """A graph of the layer, replayed with eager work between: every replay gives what the eager layer gives."""
     B = 4
