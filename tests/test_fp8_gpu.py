@@ -340,9 +340,10 @@ def append_case(lib, new, before, Hq, H, D, block, rot, interleaved, dtype, fp8,
     if not fp8:
         for x, raw, cache, got in ((kr, k64, kc, Kc), (v64, v64, vc, Vc)):
             want, tol = f64(cache).copy(), np.zeros(cache.shape)
+            allowed = u.HALF[dtype] * np.abs(x) + grow(raw) * 2.0 ** -22 + 2.0 ** -25
             for t, b, p, blk, slot in spots:
                 want[blk, :, slot] = x[t]
-                tol[blk, :, slot] = (u.HALF[dtype] * np.abs(x) + grow(raw) * 2.0 ** -22 + 2.0 ** -25)[t]
+                tol[blk, :, slot] = allowed[t]
             assert (np.abs(f64(got) - want) <= tol).all()
             assert cache is not vc or same(f64(got), want)                   # values are copied
         return
@@ -353,13 +354,13 @@ def append_case(lib, new, before, Hq, H, D, block, rot, interleaved, dtype, fp8,
             assert same(f64(got), want)
             continue
         # a turned key's fp32 error may take it over the middle between two numbers: then it is the other neighbour
-        tol = np.zeros(cache.shape)
+        tol, have, slack = np.zeros(cache.shape), f64(got), grow(raw) * 2.0 ** -22
         for t, b, p, blk, slot in spots:
             s = wants[blk][:, None]
             tol[blk, :, slot] = 2 * u.HALF[F8] * np.abs(want[blk, :, slot]) + 2.0 ** -9
-            off = np.abs(f64(got)[blk, :, slot] * s - x[t])
-            assert (off <= u.HALF[F8] * np.abs(x[t]) * 1.0001 + s * 2.0 ** -10 * 1.0001 + grow(raw)[t] * 2.0 ** -22).all()
-        diff = np.abs(f64(got) - want)
+            off = np.abs(have[blk, :, slot] * s - x[t])
+            assert (off <= u.HALF[F8] * np.abs(x[t]) * 1.0001 + s * 2.0 ** -10 * 1.0001 + slack[t]).all()
+        diff = np.abs(have - want)
         assert (diff <= tol).all() and (diff > 0).mean() < 1e-4
 
 
@@ -426,6 +427,15 @@ def test_append_is_repeatable(lib):
         assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D,block", [(64, 32), (128, 48), (64, 80), (128, 128), (64, 144), (128, 256), (64, 1024), (128, 1024)])
+def test_append_block_sizes(lib, D, block, interleaved):
+    """From one wavefront to sixteen for a (block, head): blocks filled at once, in pieces, over a border, and single tokens far into a block, with growing and falling scales."""
+    for gain in (0.01, 20.0):
+        append_case(lib, [2 * block + 5, 3, block - 1, 37], [0, block - 2, 1, block // 2], 2, 3, D, block, D // 2, interleaved, BF16, True, 51, gain=gain)
+        append_case(lib, [1, 1, 1, 0], [block - 1, block // 2 + 1, 0, 7], 1, 2, D, block, D, interleaved, FP16, True, 53, gain=gain)
+
+
 # ---- attention
 
 def attn_case(lib, lens, Hq, H, D, block, dtype, seed, scale=None, poison=True, spread=True):
@@ -475,6 +485,12 @@ def attn_case(lib, lens, Hq, H, D, block, dtype, seed, scale=None, poison=True, 
 @pytest.mark.parametrize("block", [16, 48, 64])
 def test_attn_ragged_lengths(lib, dtype, D, block):
     attn_case(lib, [1, 0, 2, 15, 16, 17, 31, 32, 33, 63, 65, 127, 129, 257, 1000, 4 * block], 6, 3, D, block, dtype, 41)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("block", [80, 256, 1024])
+def test_attn_large_blocks(lib, D, block):
+    attn_case(lib, [1, block - 1, block, block + 1, 0, 2 * block + 17], 4, 2, D, block, BF16, 42)
 
 
 @pytest.mark.parametrize("Hq,H", [(1, 1), (8, 8), (8, 1), (16, 1), (17, 1), (40, 2), (96, 3)])
