@@ -12,9 +12,10 @@
 //     dimension gets is free as long as Q's fragment agrees.
 //   * S^T leaves key 4 (l / 16) + r of query l % 16 in register r. Those are the k slots 8 (l / 16) .. + 7 of the second product
 //     (four from each half), so P needs no exchange between lanes, and the transposing LDS read fetches V for the same keys.
-// P and V are multiplied as fp16 whatever Q's type: e4m3 is exact in it, and P, at most 2^8 times the current reference
-// (which moves only when a score passes it by 8 in the log2 domain), keeps 11 bits; 2^6 on top leaves it far from fp16's small end.
-// The scale of V goes into P, divided by the largest one that the wavefront has met. The row sums take P as it is in fp32.
+// P and V are multiplied as fp16 whatever Q's type: e4m3 is exact in it. The scale of V goes into P: p = 2^(score - top) * (scale of V), `top` the running maximum of that
+// product's log2 over the wavefront's keys (it moves only when a product passes it by 8), so that a large scale on keys of little weight takes no bits from the
+// others. p is at most 2^8, 2^6 on top leaves it far from fp16's small end, and 11 bits are kept. The weights' sum has a reference of its own, the maximum of the scores,
+// and is taken in fp32 before the rounding. A scale's exponent joins the score, its mantissa multiplies.
 //
 // Keys are dealt in units to the 4 or 8 wavefronts of a workgroup and, with few (sequence, head) pairs, in ranges to several workgroups,
 // whose partial results (maximum, sum, outputs; fp32) are merged in a fixed order, by the one that comes last or by a second kernel.
@@ -36,7 +37,7 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 constexpr int PF_UNIT = 32;
 constexpr int PF_MAX_SPLIT = 64;
 constexpr int PF_LAST_SPLIT = 8;           // ranges that the last of their workgroups merges, at most
-constexpr float PF_LAZY = 8.f, PF_GAIN = 64.f;
+constexpr float PF_LAZY = 8.f, PF_GAIN = 6.f;   // log2
 
 struct PagedFp8 {
   const uint16_t* Q;
@@ -178,7 +179,8 @@ __global__ __launch_bounds__(NW * 64, 4) void paged_fp8_kernel(PagedFp8 a) {
     }
   };
 
-  float m = -__builtin_inff(), l = 0.f, top_vs = 0x1p-100f;
+  // log2 references: m of the weights (l), top of the weights times V's scales (o)
+  float m = -__builtin_inff(), l = 0.f, top = -__builtin_inff();
   f32x4 o[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -190,7 +192,7 @@ __global__ __launch_bounds__(NW * 64, 4) void paged_fp8_kernel(PagedFp8 a) {
   const uint32_t v_at = (uint32_t)(L::MAT + vrow * D + L::f(vrow) * 16 + 8 * (r16 & 1));
 
   uint32_t at = 0, next_at = 0;
-  float ks = 0.f, vs = 0.f;
+  float ks = 0.f, vm = 0.f, ve = 0.f;                      // a half's scale of K; of V, vm * 2^ve with vm in [1/2, 1)
   if (mine > 0) {
     const int hh = half_of(u0 + wave);
     at = place(hh, table[hh / hpb]);
@@ -225,7 +227,9 @@ __global__ __launch_bounds__(NW * 64, 4) void paged_fp8_kernel(PagedFp8 a) {
     }
     if (j == 0) {
       ks = *(const MLT_LDS float*)(uintptr_t)(side + 256 + lane * 4u);
-      vs = *(const MLT_LDS float*)(uintptr_t)(side + 512 + lane * 4u);
+      const float vs = *(const MLT_LDS float*)(uintptr_t)(side + 512 + lane * 4u);
+      vm = __builtin_amdgcn_frexp_mantf(vs);
+      ve = (float)__builtin_amdgcn_frexp_expf(vs);
     }
     u32x4 kr[2][KP];
 #pragma unroll
@@ -236,8 +240,9 @@ __global__ __launch_bounds__(NW * 64, 4) void paged_fp8_kernel(PagedFp8 a) {
     lds_read();
     if (j == 31) at = next_at;                           // from here on units i + 1 and later are fetched
     if (i + 1 < mine) fetch(a.Kc, at, (i + 1) & 31, ring);
-    const float kss[2] = {read_lane(ks, 2 * j), read_lane(ks, 2 * j + 1)}, vss[2] = {read_lane(vs, 2 * j), read_lane(vs, 2 * j + 1)};
-    float s[2][4], mx = -__builtin_inff();
+    const float kss[2] = {read_lane(ks, 2 * j), read_lane(ks, 2 * j + 1)}, vms[2] = {read_lane(vm, 2 * j), read_lane(vm, 2 * j + 1)},
+                ves[2] = {read_lane(ve, 2 * j), read_lane(ve, 2 * j + 1)};
+    float s[2][4];
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -261,44 +266,42 @@ __global__ __launch_bounds__(NW * 64, 4) void paged_fp8_kernel(PagedFp8 a) {
         for (int r = 0; r < 4; ++r)
           if (u * PF_UNIT + p * 16 + 4 * g + r >= len) s[p][r] = -__builtin_inff();
     }
+    float mx = -__builtin_inff(), px = -__builtin_inff();
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) mx = __builtin_fmaxf(mx, s[p][r]);
-    if (__any(mx > m + PF_LAZY)) {                       // (m = -inf: the first time)
-      float all = __builtin_fmaxf(mx, __shfl_xor(mx, 16));
-      all = __builtin_fmaxf(all, __shfl_xor(all, 32));
-      const float now = __builtin_fmaxf(m, all);
-      const float alpha = now == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - now);
-      m = now;
-      l *= alpha;
+    for (int p = 0; p < 2; ++p) {
+      const float four = __builtin_fmaxf(__builtin_fmaxf(s[p][0], s[p][1]), __builtin_fmaxf(s[p][2], s[p][3]));
+      mx = __builtin_fmaxf(mx, four);
+      px = __builtin_fmaxf(px, four + ves[p]);
+    }
+    if (__any(mx > m + PF_LAZY || px > top + PF_LAZY)) { // (-inf: the first time)
+      auto over_keys = [](float x) __attribute__((always_inline)) {
+        x = __builtin_fmaxf(x, __shfl_xor(x, 16));
+        return __builtin_fmaxf(x, __shfl_xor(x, 32));
+      };
+      auto factor = [](float was, float now) __attribute__((always_inline)) { return now == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(was - now); };
+      const float m_was = m, top_was = top;
+      m = __builtin_fmaxf(m, over_keys(mx));
+      top = __builtin_fmaxf(top, over_keys(px));
+      l *= factor(m_was, m);
+      const float alpha = factor(top_was, top);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) o[t][r] *= alpha;
     }
-    const float most = __builtin_fmaxf(vss[0], vss[1]);
-    if (most > top_vs) {
-      const float alpha = top_vs / most;
-      top_vs = most;
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) o[t][r] *= alpha;
-    }
-    const float mref = m == -__builtin_inff() ? 0.f : m, gain = PF_GAIN / top_vs;
+    const float mref = m == -__builtin_inff() ? 0.f : m, tref = top == -__builtin_inff() ? 0.f : top;
     u32x4 pf;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      const float f = vss[p] * gain;
+      const float up = ves[p] + PF_GAIN - tref;
       float e[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        e[r] = __builtin_amdgcn_exp2f(s[p][r] - mref);
-        l += e[r];
+        l += __builtin_amdgcn_exp2f(s[p][r] - mref);
+        e[r] = __builtin_amdgcn_exp2f(s[p][r] + up) * vms[p];
       }
-      pf[2 * p] = Elem<f16_tag>::pack2(e[0] * f, e[1] * f);
-      pf[2 * p + 1] = Elem<f16_tag>::pack2(e[2] * f, e[3] * f);
+      pf[2 * p] = Elem<f16_tag>::pack2(e[0], e[1]);
+      pf[2 * p + 1] = Elem<f16_tag>::pack2(e[2], e[3]);
     }
     __builtin_amdgcn_sched_barrier(0);
     // ---- outputs. Since the loads of V: those of K of the next unit
@@ -306,7 +309,7 @@ __global__ __launch_bounds__(NW * 64, 4) void paged_fp8_kernel(PagedFp8 a) {
     u32x2 vr[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-            vr[t] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((MLT_LDS i32x2*)(uintptr_t)(ring + (v_at ^ (uint32_t)(t * 16)))));
+      vr[t] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((MLT_LDS i32x2*)(uintptr_t)(ring + (v_at ^ (uint32_t)(t * 16)))));
     }
     lds_read();
     if (i + 1 < mine) fetch(a.Vc, at, (i + 1) & 31, ring + L::MAT);
@@ -339,7 +342,7 @@ __global__ __launch_bounds__(NW * 64, 4) void paged_fp8_kernel(PagedFp8 a) {
       sm[wave * 16 + r16] = m;
       sl[wave * 16 + r16] = l;
     }
-    const float f = top_vs / PF_GAIN;
+    const float f = top == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(top - PF_GAIN - m);      // back to the weights' reference
     // register r of tile t is dimension 16 t + 4 g + r
 #pragma unroll
     for (int t = 0; t < NT; ++t)
