@@ -260,7 +260,7 @@ int mlt_paged_append_fp8(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D,
  *   o = sum_j softmax_j(scale * q . k_j) v_j,   j = 0 .. seq_lens[b] - 1,   0 <= seq_lens[b] <= max_blocks * block_size
  *   Q, O          device, contiguous [B, Hq, D] of `dtype`
  *   Kc, Vc, Ks, Vs, block_table, block_size, max_blocks, num_blocks   as for mlt_paged_append_fp8
- * A sequence without keys gives zeros. The weights, each with the scale of its value, keep 11 bits whatever `dtype`, and whatever the other
+ * A sequence without keys gives zeros. The weights, each with the scale of its value, keep 22 bits whatever `dtype`, and whatever the other
  * keys' scales. Slots behind the last key are read in
  * units of 16 and ignored, as in mlt_paged_attn_decode, and so are the limits of what is read, the clamping of lengths (here
  * to 0 from below) and block numbers, and the requirements. H must divide Hq (MLT_ERR_INVALID_ARG).

@@ -79,11 +79,16 @@ def exact(q, kc, vc, ks, vs, table, lens, scale):
     return o, dict(mass=mass, most=most, reach=reach, span=span)
 
 
+def half_step(x, dtype):
+    """Half the distance of x's neighbours in `dtype` (normal numbers): what rounding costs at most."""
+    return torch.exp2(torch.floor(torch.log2(x.abs().clamp(min=2.0 ** -14)))) * HALF[dtype]
+
+
 def tolerance(o, c, n, D, dtype, rounds, weight_half):
     """|O - o| of the kernel at most.
     A score is a sum of D products in fp32, times the scales: reach (D + 4) 2^-24, and its rounding against a reference, which adds the references' size: an
     exponent of at most a = 2 reach log2(e) + 2 span + 16 in size is off by 3 a 2^-24. So is each factor by which a moved reference multiplies (one a round at most),
-    and every exp2 by 2^-22. That counts for the weights and for their sum. `weight_half`: the weights' rounding for the second product; fp16's smallest step is 2^-24,
+    and every exp2 by 2^-22. That counts for the weights and for their sum. `weight_half`: the weights' rounding for the second product, relative; fp16's smallest step is 2^-24,
     so half of it is 2^-25, against a reference of 2^GAIN times the largest weight * scale (rounded down to a power of two: half): 2^-30 of that for each key, times a value of up to 448.
     Then the fp32 sums over n keys, and the output's rounding with half of fp16's smallest step."""
     a = 2 * c["reach"] * LOG2E + 2 * c["span"] + 16
@@ -94,6 +99,12 @@ def tolerance(o, c, n, D, dtype, rounds, weight_half):
 
 CASES = [("rise", 3.0), ("rise", 12.0), ("fall", 12.0), ("scales_rise", 3.0), ("scales_rise", 13.0), ("scales_fall", 13.0), ("across", 3.0), ("across", 11.0),
          ("light_first", 20.0), ("light_first", 28.0), ("light_first", 40.0), ("light_last", 28.0), ("light_last", 40.0)]
+
+
+def two_halves(p):
+    """p as the kernel multiplies with it: rounded to fp16, and what that left, rounded."""
+    hi = np.float16(p).astype(float)
+    return hi + np.float16(p - hi).astype(float)
 
 
 def emulate(q, k, ks, v, vs, scale, waves, n, wrong=""):
@@ -120,7 +131,7 @@ def emulate(q, k, ks, v, vs, scale, waves, n, wrong=""):
                     o *= big[-2] / big[-1]
                 o = o + np.float16(2.0 ** (s - top + GAIN) * (vs[u] / big[-1])).astype(float) @ v[u]
             else:
-                o = o + np.float16(2.0 ** (s + ex + GAIN - top) * mant).astype(float) @ v[u]
+                o = o + two_halves(2.0 ** (s + ex + GAIN - top) * mant) @ v[u]
             l += (2.0 ** (s - m)).sum()
         last = np.max(vs[w::waves]) if wrong == "scale reference" else 1.0
         parts.append((m, l, o * last * 2.0 ** (top - GAIN - m) if m > -math.inf else o))

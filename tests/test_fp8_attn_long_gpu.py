@@ -10,7 +10,7 @@ from test_fp8_debug_gpu import _stream, both, dbg  # noqa: F401  (fixtures)
 
 pytestmark = pytest.mark.gpu
 BF16, FP16 = torch.bfloat16, torch.float16
-WEIGHT_HALF = 2.0 ** -11                                                  # the weights' 11 bits in the second product
+WEIGHT_HALF = 2.0 ** -22                                                  # the weights in the second product: 11 bits, and 11 of what they leave
 
 
 @pytest.fixture(autouse=True)

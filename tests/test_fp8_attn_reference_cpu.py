@@ -13,7 +13,7 @@ def _run(kind, step, dtype, wrong=""):
     c = a.units_case(kind, step, WAVES, ROUNDS, D, dtype, 3)
     n = int(c["lens"])
     o, more = a.exact(**c)
-    tol = a.tolerance(o, more, n, D, dtype, ROUNDS, 2.0 ** -11)[0].numpy()
+    tol = a.tolerance(o, more, n, D, dtype, ROUNDS, 2.0 ** -22)[0].numpy()
     at = c["table"][0].long()
     k, v, ks, vs = (c[x][at].double().numpy() for x in ("kc", "vc", "ks", "vs"))
     o = o[0].numpy()

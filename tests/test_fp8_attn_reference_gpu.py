@@ -6,7 +6,7 @@ import fp8_attn_util as a
 
 pytestmark = pytest.mark.gpu
 BF16, FP16 = torch.bfloat16, torch.float16
-WEIGHT_HALF = 2.0 ** -11                                                  # the weights' 11 bits in the second product
+WEIGHT_HALF = 2.0 ** -22                                                  # the weights in the second product: 11 bits, and 11 of what they leave
 
 
 @pytest.fixture(autouse=True)
@@ -75,3 +75,26 @@ def test_references_move_with_four_wavefronts(lib, key_split, kind, step, dtype,
     tol = a.tolerance(o, more, int(one["lens"]), D, dtype, 6, WEIGHT_HALF)
     assert bool((tol < 0.1 * o.abs()).all()) and bool(((O[:1].double() - o).abs() <= tol).all())
     assert torch.equal(O, O[:1].expand_as(O))
+
+
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -12])
+@pytest.mark.parametrize("D", [64, 128])
+def test_weights_keep_22_bits(lib, D, scale):
+    """Few keys, (nearly) equal scores and value scales of any mantissa, positive values: nothing averages out, and a weight of 11 bits would show beside the
+    output's rounding. The bound is that of `tolerance` with 2^-22 for the weights (11 bits, and 11 of what they leave) and half the output's own step instead of half
+    of the largest relative one."""
+    g = torch.Generator().manual_seed(17)
+    H, G, block = 4, 2, 16
+    lens = [1, 2, 5, 16, 17, 31, 32, 33, 64, 100]
+    nb = len(lens) * 7
+    kc, vc = (torch.randn((nb, H, block, D), generator=g).mul_(60).abs().add_(8).to(a.F8) for _ in range(2))
+    ks, vs = (torch.exp2(torch.rand((nb, H), generator=g) * 3 - 8) for _ in range(2))
+    c = on_gpu(dict(q=torch.randn((len(lens), H * G, D), generator=g).to(FP16), kc=kc, vc=vc, ks=ks, vs=vs, scale=scale,
+                    table=torch.randperm(nb, generator=g).to(torch.int32).reshape(len(lens), 7).contiguous(), lens=torch.tensor(lens, dtype=torch.int32)))
+    O = run(lib, c)
+    o, more = a.exact(**c)
+    n = c["lens"].double()[:, None, None]
+    tol = a.tolerance(o, more, n, D, FP16, 1, WEIGHT_HALF) - (a.HALF[FP16] * o.abs() - a.half_step(o, FP16))
+    err = (O.double() - o).abs()
+    print("   worst %.2f of the tolerance, %.3f of the results beyond it" % (float((err / tol).max()), float((err > tol).double().mean())), flush=True)
+    assert bool((tol < 1.5 * a.half_step(o, FP16)).all()) and bool((err <= tol).all())
