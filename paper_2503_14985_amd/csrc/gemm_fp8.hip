@@ -337,10 +337,10 @@ __global__ __launch_bounds__(G8_NT, 2) void gemm_fp8_kp_kernel(int M, int N, int
   const int a_last = M - 1 - m0, b_last = N - 1 - n0;
   const bool stream_a = nbn == 1, stream_b = nbm == 1;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr_t)smem;
-  const uint32_t srow = (uint32_t)((m0 + 64 * w + lane < M ? m0 + 64 * w + lane : M - 1) * 4);
+  const uint32_t srow = (uint32_t)(64 * w + lane <= a_last ? 64 * w + lane : a_last) * 4u;   // inside the tile: from row 0 on it would pass 32 bits
   auto issue = [&](int s, int stage, auto&& between) __attribute__((always_inline)) {
     const uint32_t at = lds0 + stage * T::STAGE;
-    load_lds4(Sa + (int64_t)(kb0 + s) * ldsa, srow, at + T::A_B + T::B_B + w * 256);
+    load_lds4(Sa + (int64_t)(kb0 + s) * ldsa + m0, srow, at + T::A_B + T::B_B + w * 256);
     load_blocks<NLA, TAIL>(a_base + (int64_t)s * F8_KB, (uint32_t)lda, a_last, w * NLA, at + w * (NLA * 1024), lane, stream_a, K - s * F8_KB, between);
     load_blocks<NLB, TAIL>(b_base + (int64_t)s * F8_KB, (uint32_t)ldb, b_last, w * NLB, at + T::A_B + w * (NLB * 1024), lane, stream_b, K - s * F8_KB,
                            [&](int i) __attribute__((always_inline)) { between(NLA + i); });
