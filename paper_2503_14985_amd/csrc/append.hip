@@ -288,7 +288,7 @@ template <typename Tag, int D, bool FP8, bool NEIGHBOURS, int W>
 int launch_append_w(Append a, int64_t rows, int64_t units, hipStream_t s) {
   constexpr int WAVES = ap_threads(W) / 64;
   const int64_t row_blocks = rows ? ((int64_t)a.T * a.parts + WAVES - 1) / WAVES : 0, unit_blocks = (units * W + WAVES - 1) / WAVES;
-  if (row_blocks + unit_blocks > 0x7fffffff || unit_blocks * WAVES > 0x7fffffff) return MLT_ERR_UNSUPPORTED;      // units are counted in 32 bits
+  if (!launch_fits(row_blocks + unit_blocks, WAVES * 64)) return MLT_ERR_UNSUPPORTED;      // (with it wavefronts, and units, are counted in 32 bits)
   if (row_blocks + unit_blocks == 0) return MLT_OK;
   a.row_blocks = (int)row_blocks;
   hipLaunchKernelGGL((append_kernel<Tag, D, FP8, NEIGHBOURS, W>), dim3((unsigned)(row_blocks + unit_blocks)), dim3(WAVES * 64), 0, s, a);

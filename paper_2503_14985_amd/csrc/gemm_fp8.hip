@@ -512,6 +512,7 @@ int launch_fp8(const GemmFp8Args& a, hipStream_t s) {
   auto kern = gemm_fp8_kernel<Tag, BT, TAIL>;
   static thread_local int configured_dev = -1;          // opt in to > 64 KB LDS once per device
   int dev = 0;
+  const int64_t nbm = (a.M + BT - 1) / BT, nbn = (a.N + BT - 1) / BT;
   if (hipGetDevice(&dev) != hipSuccess) return MLT_ERR_DEVICE;
   if (configured_dev != dev) {
     if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, SMEM) != hipSuccess) {
@@ -520,8 +521,6 @@ int launch_fp8(const GemmFp8Args& a, hipStream_t s) {
     }
     configured_dev = dev;
   }
-  const int64_t nbm = (a.M + BT - 1) / BT, nbn = (a.N + BT - 1) / BT;
-  if (nbm * nbn > 0x7fffffff) return MLT_ERR_UNSUPPORTED;
   hipLaunchKernelGGL(kern, dim3((unsigned)(nbm * nbn)), dim3(G8_NT), SMEM, s, (int)a.M, (int)a.N, (int)a.K, a.A, a.lda, a.Sa, a.ldsa, a.B, a.ldb, a.Sb, a.ldsb, a.C,
                      a.ldc, (int)nbm, (int)nbn, device_xcds());
   return hipGetLastError() == hipSuccess ? MLT_OK : MLT_ERR_LAUNCH;
@@ -547,7 +546,6 @@ int launch_fp8_kp(const GemmFp8Args& a, int parts, float* part, hipStream_t s) {
     configured_dev = dev;
   }
   const int64_t nbm = (a.M + BM - 1) / BM, nbn = (a.N + 127) / 128;
-  if (nbm * nbn * parts > 0x7fffffff) return MLT_ERR_UNSUPPORTED;
   const int KT = (int)((a.K + F8_KB - 1) / F8_KB), part_steps = parts > 1 ? (KT + parts - 1) / parts : 0;
   const bool joined = parts == 2 && part_steps < KT;     // (as part_bytes has it)
   if (parts > 1) parts = (KT + part_steps - 1) / part_steps;                // no empty part
@@ -623,8 +621,12 @@ Fp8Plan plan_fp8(const GemmFp8Args& a, int max_parts, int64_t ncu) {
   const int forced = known(a.forced) ? a.forced : GEMM_AUTO;
   Fp8Plan best{forced == GEMM_AUTO ? GEMM_256_PP16 : forced, 1};
   double least = 1e30;
+  auto workgroups = [&](int v, int parts) {
+    return v == GEMM_256_PP16 ? (a.M + 255) / 256 * ((a.N + 255) / 256) : v == GEMM_128_PP16 ? (a.M + 127) / 128 * ((a.N + 127) / 128) : kp_tiles(v, a) * parts;
+  };
   auto offer = [&](int v, int parts) {
     if (forced != GEMM_AUTO && v != forced) return;
+    if (v != GEMM_SKINNY && !launch_fits(workgroups(v, parts), G8_NT)) return;
     if (parts == 2 && v != GEMM_SKINNY && kp_tiles(v, a) > kScratchCounters) return;       // a counter for each tile
     if (parts > 1 && a.forced_parts == 0 && part_bytes(Fp8Plan{v, parts}, a) > kStaticScratchBytes) return;
     const double t = fp8_estimate(v, parts, a.M, a.N, a.K, ncu);
@@ -639,7 +641,13 @@ Fp8Plan plan_fp8(const GemmFp8Args& a, int max_parts, int64_t ncu) {
     offer(GEMM_256_PP16, 1);
     offer(GEMM_128_PP16, 1);
   }
-  return best;
+  if (least < 1e30) return best;
+  // nothing that was asked for can be launched: without the parts, then without the kernel
+  GemmFp8Args b = a;
+  if (a.forced_parts > 1) b.forced_parts = 1;
+  else if (forced != GEMM_AUTO) b.forced = GEMM_AUTO;
+  else return Fp8Plan{GEMM_AUTO, 0};
+  return plan_fp8(b, max_parts, ncu);
 }
 
 template <typename Tag>
@@ -652,6 +660,7 @@ int run_fp8_t(const GemmFp8Args& a, hipStream_t s, char* name, size_t size) {
   DeviceInfo di;
   const int64_t ncu = device_info(di) && di.ncu > 0 ? di.ncu : 256;
   Fp8Plan p = plan_fp8(a, 8, ncu);
+  if (p.parts == 0) return MLT_ERR_UNSUPPORTED;          // more workgroups than a launch can have, whatever the tile
   float* part = nullptr;
   if (p.parts > 1) {
     part = cached_scratch(part_bytes(p, a), s);

@@ -181,7 +181,10 @@ int run_paged_decode(const PagedArgs& a, hipStream_t s, int* nsplit_out);
 int plan_paged_split(const PagedArgs& a);                                       // key ranges per (sequence, head)
 bool paged_by_length(const PagedArgs& a, int64_t nsplit, int64_t ncu);   // workgroups dealt out by sequence length?
 
-// The 8-bit operators (arguments as in include/mlt.h)
+// A launch counts its work-items in 32 bits a dimension; one of more wraps and leaves workgroups out, without an error.
+inline bool launch_fits(int64_t workgroups, int64_t threads) { return workgroups <= 0xffffffffll / threads; }
+
+// The 8-bit operators (arguments as in include/mlt.h). What they cannot launch they refuse, with nothing enqueued and before they use the device.
 struct QuantArgs {
   int64_t M, K;
   const uint16_t* X; int64_t ldx;

@@ -501,7 +501,9 @@ int run_paged_fp8(const PagedFp8Args& a, hipStream_t s, int* nsplit_out, int* wa
   DeviceInfo di;
   const int64_t ncu = device_info(di) && di.ncu > 0 ? di.ncu : 256;
   const int tiles = (int)((a.Hq / a.H + 15) / 16);
+  if (!launch_fits(a.B * a.H * tiles, 256)) return MLT_ERR_UNSUPPORTED;    // (the wider form is for few workgroups)
   int nsplit = plan_paged_fp8_split(a, a.B * a.H * tiles, ncu);
+  if (!launch_fits(a.B * a.Hq, 256)) nsplit = 1;         // (what the merging kernel would need)
   float* part = nullptr;
   if (nsplit > 1) {
     part = cached_scratch(a.B * a.Hq * nsplit * (2 + a.D) * (int64_t)sizeof(float), s);

@@ -118,7 +118,7 @@ template <typename Tag>
 int run_quant_t(const QuantArgs& a, hipStream_t s) {
   constexpr int RPW = 4;
   const int64_t cols = a.block_rows == 1 ? 512 : F8_KB, rows = a.block_rows == 1 ? 4 * RPW : 128, nbx = (a.K + cols - 1) / cols, wgs = nbx * ((a.M + rows - 1) / rows);
-  if (wgs > 0x7fffffff) return MLT_ERR_UNSUPPORTED;
+  if (!launch_fits(wgs, QT_NT)) return MLT_ERR_UNSUPPORTED;
   if (a.block_rows == 1)
     hipLaunchKernelGGL((quant_rows_kernel<Tag, RPW>), dim3((unsigned)wgs), dim3(QT_NT), 0, s, (int)a.M, (int)a.K, a.X, a.ldx, a.Xq, a.ldq, a.S, a.lds, (int)nbx);
   else
