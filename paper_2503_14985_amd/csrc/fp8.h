@@ -18,15 +18,15 @@ __device__ __forceinline__ float pow2_scale(float amax) {
   e = e < 27 ? 27 : e;
   return __builtin_bit_cast(float, e << 23);
 }
-// the smallest power of two >= s in the same range (anything that is no positive number: its lower end)
+// the smallest power of two >= s in 2^-100 .. 2^126, whose inverse is a normal number (anything that is no positive number: the lower end)
 __device__ __forceinline__ float pow2_ceil(float s) {
   if (!(s > 0.f)) return __builtin_bit_cast(float, 27 << 23);
   const int bits = __builtin_bit_cast(int, s);
   int e = (bits >> 23) + ((bits & 0x7fffff) ? 1 : 0);
-  e = e < 27 ? 27 : e > 247 ? 247 : e;
+  e = e < 27 ? 27 : e > 253 ? 253 : e;
   return __builtin_bit_cast(float, e << 23);
 }
-// 1 / s of a power of two of that range: a power of two as well
+// 1 / s of a power of two of either range: a power of two as well
 __device__ __forceinline__ float pow2_inv(float s) { return __builtin_bit_cast(float, (254 << 23) - __builtin_bit_cast(int, s)); }
 // |x| of a finite x, else 0
 __device__ __forceinline__ float finite_abs(float x) {
