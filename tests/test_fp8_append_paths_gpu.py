@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import fp8_util as u
+from test_fp8_gpu import append_case
 
 pytestmark = pytest.mark.gpu
 BF16, FP16, F8 = torch.bfloat16, torch.float16, u.F8
@@ -52,3 +53,31 @@ def test_scales_at_the_ends_of_their_range(lib, exponent):
         assert np.isfinite(want).all()
         assert np.array_equal(f64(gots), wants), (f64(gots), wants)
         assert np.array_equal(f64(got), want)
+
+
+# ---- a prefill's rows: four accesses of a token at once, with 16 or more heads of 128 and 2048 or more tokens
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("fp8,Hq,H", [(True, 16, 1), (True, 17, 2), (True, 19, 1), (True, 32, 8), (True, 33, 1), (False, 12, 2), (False, 9, 4), (False, 5, 7), (False, 0, 8), (False, 14, 3),
+                                      (False, 40, 3)])
+def test_prefill_rows(lib, fp8, Hq, H, interleaved):
+    """Heads that fill the accesses and heads that do not, which of a token's rows are queries, keys and values falling anywhere in them; padding rows at the end."""
+    new, before = [1300, 0, 1, 740, 9], [5, 40, 16, 0, 31]
+    append_case(lib, new, before, Hq, H, 128, 16, 128, interleaved, BF16, fp8, 19, pad=6)
+    assert sum(new) >= 2048
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("rot", [0, 16, 96])
+def test_prefill_rows_partly_turned(lib, fp8, rot):
+    append_case(lib, [2048, 3], [7, 0], 20, 2, 128, 32, rot, False, FP16, fp8, 23)
+
+
+def test_prefill_rows_without_a_place(lib):
+    """Positions past the table of angles and block numbers outside the cache, in the same loop."""
+    def bad(t):
+        t = t.clone()
+        t[0, 3], t[1, 1] = -1, 1 << 30
+        return t
+    for fp8 in (False, True):
+        append_case(lib, [1900, 200], [0, 4], 16, 2, 128, 16, 128, False, BF16, fp8, 29, tables=bad, positions=700)
