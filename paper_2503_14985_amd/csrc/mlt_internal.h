@@ -235,6 +235,7 @@ struct PagedFp8Args {
   int dtype;
   int forced_split = 0;      // as in PagedArgs
 };
+bool paged_fp8_by_length(const PagedFp8Args& a, int64_t wgs, int64_t nsplit, bool wide, int64_t ncu);   // wgs workgroups (wide: of 512 threads) dealt out by sequence length?
 int run_paged_fp8(const PagedFp8Args& a, hipStream_t s, int* nsplit_out, int* waves_out);   // paged_fp8.hip; key ranges per pair and wavefronts per workgroup that ran
 
 // The library's own scratch memory for a stream of the current device: at least `bytes`, behind its counters, kept

@@ -497,6 +497,16 @@ int plan_paged_fp8_split(const PagedFp8Args& a, int64_t wgs, int64_t ncu) {
 
 }  // namespace
 
+// Whether workgroups are dealt out by sequence length, as the 16-bit form does. Every one of them then ranks the batch, whose lengths have to fit its threads: 1 us with 64
+// sequences, 3 with 192, 5 with 250. It pays where there is much to read for each, 256 KiB a workgroup and 2 KiB a sequence. us in batch order / by length, for lengths from a
+// quarter of that on and for equal ones, D = 128: 64 x 8 pairs of at most 4096 keys 64.5 / 54.0 (82.3 / 83.4 equal), 70 x 8 72.0 / 64.6 (106.5 / 108.0), 128 x 8 116.8 / 108.0
+// (165.0 / 168.9), 250 x 4 120.5 / 108.5 (161.6 / 169.4); 250 x 2 of 8192 122.3 / 106.7 (160.4 / 165.3). On the other side: 250 x 8 of 1024 59.1 / 60.8 (83.7 / 88.9),
+// 192 x 4 of 1024 27.4 / 27.5 (33.7 / 37.2), 128 x 8 of 512 19.3 / 19.7 (24.1 / 25.9).
+bool paged_fp8_by_length(const PagedFp8Args& a, int64_t wgs, int64_t nsplit, bool wide, int64_t ncu) {
+  const int64_t kib = a.max_blocks * a.block_size / nsplit * a.D * 2 / 1024;
+  return a.B >= 2 && a.B <= (wide ? 512 : 256) && wgs > ncu && kib >= 256 && kib >= 2 * a.B;
+}
+
 int run_paged_fp8(const PagedFp8Args& a, hipStream_t s, int* nsplit_out, int* waves_out) {
   DeviceInfo di;
   const int64_t ncu = device_info(di) && di.ncu > 0 ? di.ncu : 256;
@@ -513,10 +523,7 @@ int run_paged_fp8(const PagedFp8Args& a, hipStream_t s, int* nsplit_out, int* wa
   // 8 wavefronts where two workgroups a CU or fewer take all the keys (64 sequences of 4096 keys, D = 64: 31.5 us, with 4 wavefronts 34.1), otherwise 4,
   // which leave a CU more workgroups to choose from (128 sequences of 512 keys: 18.3 us, with 8 wavefronts 20.2).
   const bool wide = wgs <= 2 * ncu;
-  // Dealt out by sequence length, as the 16-bit form does: 64 sequences of 1 to 4096 keys 56.2 us, 63.4 without (all of 4000 keys: 84.0 and 83.3). Every workgroup
-  // then ranks the batch, 1 to 2 us, so it takes few sequences and much to read for each (128 sequences of 512 keys: 19.3 us, 18.2 without).
-  const bool by_length = a.B >= 2 && a.B <= 64 && wgs > ncu && a.max_blocks * a.block_size / nsplit * a.D * 2 >= 256 * 1024;
-  const int order = by_length ? (int)ncu : 0;
+  const int order = paged_fp8_by_length(a, wgs, nsplit, wide, ncu) ? (int)ncu : 0;
   *nsplit_out = nsplit;
   *waves_out = wide ? 8 : 4;
   if (a.dtype == MLT_BF16)

@@ -130,3 +130,28 @@ def test_long_sequences_agree_with_the_debug_build(dbg, both, lens, Hq, H, D, bl
             assert dbg.mlt_paged_attn_decode_fp8(len(lens), Hq, H, D, block, c["table"].shape[1], c["kc"].shape[0], *at, got.data_ptr(), c["scale"], code, _stream()) == 0
             assert dbg.mlt_last_kernel().decode() == name
             assert torch.equal(got.view(torch.int16), want.view(torch.int16)), name
+
+
+def mixed(B, s):
+    """Lengths from s / 4 to s out of order, with empty sequences, single keys and equal lengths among them."""
+    lens = [s // 4 + (s - s // 4) * i // (B - 1) for i in range(B)]
+    lens = [lens[37 * i % B] if B % 37 else lens[i] for i in range(B)]
+    lens[3], lens[B // 2], lens[5] = 0, 1, lens[6]
+    return lens
+
+
+@pytest.mark.parametrize("B,s,Hq,H,D,block", [(70, 4100, 16, 8, 128, 16), (70, 8192, 8, 8, 64, 32), (128, 1100, 8, 8, 128, 16), (250, 4096, 4, 4, 64, 64), (256, 2100, 3, 3, 128, 16),
+                                              (300, 4097, 1, 1, 128, 16), (512, 8200, 1, 1, 64, 128)])
+def test_large_mixed_batches_dealt_by_length(lib, dbg, both, B, s, Hq, H, D, block):  # noqa: F811
+    """More sequences than a wavefront has lanes (up to one for each thread of a workgroup), the longest with more than 32 units to a wavefront; and the debug build's bits."""
+    lens = mixed(B, s)
+    c = long_case(B, lens, Hq, H, D, block, BF16, B + s)
+    O = check(lib, c)
+    assert bool((O[3] == 0).all())
+    both(split=1)
+    want = run(lib, c)
+    at = [c[x].data_ptr() for x in ("q", "kc", "vc", "ks", "vs", "table", "lens")]
+    for _ in range(2):
+        got = torch.full_like(O, float("nan"))
+        assert dbg.mlt_paged_attn_decode_fp8(B, Hq, H, D, block, c["table"].shape[1], c["kc"].shape[0], *at, got.data_ptr(), c["scale"], 0, _stream()) == 0
+        assert torch.equal(got.view(torch.int16), want.view(torch.int16))
