@@ -43,7 +43,8 @@ typedef enum { MLT_BF16 = 0, MLT_FP16 = 1 } mlt_dtype;
 typedef enum {
   MLT_OK = 0,
   MLT_ERR_INVALID_ARG = -1, /* null pointer, negative size, leading dimension too small, bad dtype */
-  MLT_ERR_UNSUPPORTED = -2, /* valid request with no kernel (e.g. head dimension not 64 or 128) */
+  MLT_ERR_UNSUPPORTED = -2, /* valid request with no kernel (e.g. head dimension not 64 or 128; sizes that would take a launch of more
+                               than 2^32 work-items, some 10^7 workgroups) */
   MLT_ERR_LAUNCH = -3,      /* the HIP runtime rejected the kernel launch */
   MLT_ERR_DEVICE = -4,      /* no usable gfx950 device is current */
   MLT_ERR_SCRATCH = -5      /* mlt_gemm_noalloc: the call needs more than the fixed scratch array holds */
@@ -181,7 +182,6 @@ int mlt_paged_attn_decode(int64_t B, int64_t H, int64_t D, int64_t block_size, i
  * element. A number is its e4m3 value times the fp32 scale of its block. The scales that the library writes are powers of
  * two: the smallest s >= 2^-100 with max |x| <= 448 s over the block's finite x, so that the rounding to e4m3 (to nearest, ties to
  * even) is the only one. Infinities and NaN become NaN. The scales that it reads may be any numbers from 2^-100 to 2^126.
- * Sizes that would take a launch of more than 2^32 work-items (some 10^7 workgroups) are MLT_ERR_UNSUPPORTED.
  */
 
 /*

@@ -79,8 +79,7 @@ __global__ __launch_bounds__(256) void gemm_general_kernel(
 
 // K == 0: the empty sum (only launched when C is overwritten; C += 0 is a no-op).
 __global__ void gemm_zero_kernel(int M, int N, uint16_t* __restrict__ C, int64_t ldc) {
-  const int64_t e = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (e < (int64_t)M * N) C[(e / N) * ldc + (e % N)] = 0;
+  for (int64_t e = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; e < (int64_t)M * N; e += (int64_t)gridDim.x * blockDim.x) C[(e / N) * ldc + (e % N)] = 0;
 }
 
 // ------------------------------------------------------------------------------------------
@@ -88,6 +87,7 @@ __global__ void gemm_zero_kernel(int M, int N, uint16_t* __restrict__ C, int64_t
 // ------------------------------------------------------------------------------------------
 template <typename Tag>
 static int launch_general(const GemmArgs& g, hipStream_t s) {
+  if (!launch_fits((g.N + 63) / 64, 256)) return MLT_ERR_UNSUPPORTED;
   dim3 grid((unsigned)((g.N + 63) / 64), (unsigned)((g.M + 63) / 64));
   hipLaunchKernelGGL(gemm_general_kernel<Tag>, grid, dim3(256), 0, s, (int)g.M, (int)g.N, (int)g.K,
                      g.A, g.lda, g.B, g.ldb, g.transB, g.C, g.ldc, g.epi(), g.bias);
@@ -478,8 +478,8 @@ static int run_gemm_t(const GemmArgs& g, const GemmPlan& p, hipStream_t s) {
   switch (p.variant) {
     case GEMM_ZERO: {
       if (g.acc32) return MLT_OK;
-      const int64_t n = g.M * g.N;
-      hipLaunchKernelGGL(gemm_zero_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s,
+      const int64_t wgs = (g.M * g.N + 255) / 256;
+      hipLaunchKernelGGL(gemm_zero_kernel, dim3((unsigned)(wgs < 1 << 20 ? wgs : 1 << 20)), dim3(256), 0, s,
                          (int)g.M, (int)g.N, g.C, g.ldc);
       return hipGetLastError() == hipSuccess ? MLT_OK : MLT_ERR_LAUNCH;
     }

@@ -329,6 +329,7 @@ template <typename Tag, bool TRANSB, int BM, int BN, bool TAIL>
 static int launch_kp(const GemmArgs& g, hipStream_t s) {
   constexpr int SMEM = KpTile<BM, BN>::SMEM;
   auto kern = gemm_kp_kernel<Tag, TRANSB, BM, BN, TAIL>;
+  if (!launch_fits((g.M + BM - 1) / BM * ((g.N + BN - 1) / BN) * (g.parts > 1 ? g.parts : 1), KP_NT)) return MLT_ERR_UNSUPPORTED;
   static thread_local int configured_dev = -1;          // opt in to > 64 KB LDS once per device
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return MLT_ERR_DEVICE;

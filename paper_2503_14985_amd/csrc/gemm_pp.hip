@@ -370,6 +370,7 @@ template <typename Tag, bool TRANSB, int MS, int BT, int BK, bool TAIL>
 static int launch_pp_k(const GemmArgs& g, hipStream_t s) {
   constexpr int PP_BM = BT, PP_BN = BT, PP_SMEM = PpTile<BT, BK>::SMEM;
   auto kern = gemm_pp_kernel<Tag, TRANSB, MS, BT, BK, TAIL>;
+  if (!launch_fits((g.M + PP_BM - 1) / PP_BM * ((g.N + PP_BN - 1) / PP_BN), PP_NT)) return MLT_ERR_UNSUPPORTED;
   static thread_local int configured_dev = -1;          // opt in to > 64 KB LDS once per device
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return MLT_ERR_DEVICE;

@@ -482,6 +482,7 @@ static int launch_tile(const GemmArgs& g, hipStream_t s) {
   typedef GemmTile<Tag, BM, BN, BK, WM, WN, TRANSB> Cfg;
   static_assert(Cfg::NT * KS <= 1024 && KS * Cfg::SMEM <= 160 * 1024, "one workgroup, one CU's LDS");
   auto kern = gemm_tile_kernel<Tag, BM, BN, BK, WM, WN, TRANSB, KS, AL, ACC>;
+  if (!launch_fits((g.M + BM - 1) / BM * ((g.N + BN - 1) / BN), Cfg::NT * KS)) return MLT_ERR_UNSUPPORTED;
   static thread_local int configured_dev = -1;          // opt in to > 64 KB LDS once per device
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return MLT_ERR_DEVICE;

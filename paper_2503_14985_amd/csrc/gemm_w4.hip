@@ -250,6 +250,7 @@ __global__ __launch_bounds__(W4_NT) void gemm_w4_kernel(
 template <typename Tag, bool TRANSB>
 static int launch_w4(const GemmArgs& g, hipStream_t s) {
   auto kern = gemm_w4_kernel<Tag, TRANSB>;
+  if (!launch_fits((g.M + W4_BM - 1) / W4_BM * ((g.N + W4_BN - 1) / W4_BN), W4_NT)) return MLT_ERR_UNSUPPORTED;
   static thread_local int configured_dev = -1;          // opt in to > 64 KB LDS once per device
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return MLT_ERR_DEVICE;

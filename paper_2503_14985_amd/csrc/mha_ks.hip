@@ -406,6 +406,8 @@ template <typename Tag, int D, int QW, bool SPLIT, bool CAUSAL>
 int launch_ks(const MhaArgs& a, int nsplit, float* scratch, hipStream_t s) {
   typedef KsCfg<D, QW> L;
   auto kern = mha_ks_kernel<Tag, D, QW, SPLIT, CAUSAL>;
+  const int64_t nq = (a.Sq + L::BM - 1) / L::BM, total = a.B * a.H * nq, rows = a.B * a.H * a.Sq;
+  if (!launch_fits(total, 512) || (SPLIT && !launch_fits(rows * (D / 8) / 256 + 1, 256))) return MLT_ERR_UNSUPPORTED;
   static thread_local int configured_dev = -1;          // opt in to > 64 KB LDS once per device
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return MLT_ERR_DEVICE;
@@ -416,8 +418,6 @@ int launch_ks(const MhaArgs& a, int nsplit, float* scratch, hipStream_t s) {
     }
     configured_dev = dev;
   }
-  const int64_t nq = (a.Sq + L::BM - 1) / L::BM, total = a.B * a.H * nq, rows = a.B * a.H * a.Sq;
-  if (total > 0x7fffffff) return MLT_ERR_UNSUPPORTED;
   float c = (a.scale < 0 ? -a.scale : a.scale) * 1.4426950408889634f;   // c > 0 always, as in launch_mha_pp
   if (c < 1e-30f) c = 1e-30f;
   float* ps = SPLIT ? scratch + (int64_t)nsplit * rows * D : nullptr;

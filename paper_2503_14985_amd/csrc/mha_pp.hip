@@ -1202,6 +1202,9 @@ template <typename Tag, int D, bool CAUSAL, int MS>
 int launch_mha_pp(const MhaArgs& a, hipStream_t s) {
   typedef PaCfg<D> L;
   auto kern = MS == 16 ? mha_pp16_kernel<Tag, D, CAUSAL> : mha_pp_kernel<Tag, D, CAUSAL>;
+  const int nq = (int)((a.Sq + PA_BM - 1) / PA_BM);
+  const int64_t total = a.B * a.H * nq;
+  if (!launch_fits(total, PA_NT)) return MLT_ERR_UNSUPPORTED;
   static thread_local int configured_dev = -1;          // opt in to > 64 KB LDS once per device
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return MLT_ERR_DEVICE;
@@ -1213,9 +1216,6 @@ int launch_mha_pp(const MhaArgs& a, hipStream_t s) {
     }
     configured_dev = dev;
   }
-  const int nq = (int)((a.Sq + PA_BM - 1) / PA_BM);
-  const int64_t total = a.B * a.H * nq;
-  if (total > 0x7fffffff) return MLT_ERR_UNSUPPORTED;
   const float LOG2E = 1.4426950408889634f;
   // c > 0 always: a zero scale becomes a positive one too small to move any weight off 1, which
   // keeps (-inf) * c = -inf for masked scores instead of NaN

@@ -309,6 +309,7 @@ __global__ __launch_bounds__(4 * D) void paged_merge_kernel(const float* __restr
 
 template <typename Tag, int D>
 int launch_paged(const PagedArgs& a, int nsplit, float* part, hipStream_t s) {
+  if (!launch_fits(a.B * a.H, nsplit > 1 ? 4 * D : PG_NT)) return MLT_ERR_UNSUPPORTED;
   const float c = a.scale * 1.4426950408889634f;
   const unsigned pairs = (unsigned)(a.B * a.H);
   DeviceInfo di;

@@ -17,6 +17,6 @@ def test_launches_past_2_32_work_items_are_refused(tmp_path):
     r = subprocess.run([HIPCC, "-O1", "-std=c++17", "--offload-arch=gfx950", "-x", "hip", os.path.join(ROOT, "tests", "host", "fp8_limits_driver.cpp"),
                         "-x", "none", "-o", exe, os.path.join(LIB_DIR, "libmlt.so"), "-Wl,-rpath," + LIB_DIR], capture_output=True, text=True, timeout=600)
     assert r.returncode == 0, r.stderr[-3000:]
-    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120, env=dict(os.environ, HIP_VISIBLE_DEVICES="-1"))
     assert r.returncode == 0, r.stderr[-2000:]
     assert r.stdout.split() == ["-2"] * 12, r.stdout            # MLT_ERR_UNSUPPORTED
