@@ -253,6 +253,17 @@ def _stream(stream, device) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """An output that the call allocates itself: memory of the stream that the call goes to. The current stream's may still have an earlier tensor's
+    work pending on it, and its next tensor may take it while the call is pending."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=device) if int(stream) else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 class _OtherDevice:
     """torch.cuda.device, entered only when `device` is not the current one: its enter and exit, and
     torch.cuda.current_stream() beside them, took 6 of the 11 us of a small call (2000 calls of
@@ -280,7 +291,7 @@ def _rows_contiguous(t: torch.Tensor, name: str) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-def _gemm_operands(name: str, A, B, C, transB: bool, c_dtype=None):
+def _gemm_operands(name: str, A, B, C, transB: bool, c_dtype=None, stream=None):
     """Shapes, dtype code and leading dimensions of a GEMM call (C allocated when None): the
     marshalling every GEMM entry point shares."""
     if not (A.is_cuda and B.is_cuda and (C is None or C.is_cuda)):
@@ -294,7 +305,7 @@ def _gemm_operands(name: str, A, B, C, transB: bool, c_dtype=None):
         raise ValueError("inner dimensions differ: %d vs %d" % (K, Kb))
     c_dtype = A.dtype if c_dtype is None else c_dtype
     if C is None:
-        C = torch.empty((M, N), dtype=c_dtype, device=A.device)
+        C = _empty((M, N), c_dtype, A.device, stream)
     elif C.dtype != c_dtype or tuple(C.shape) != (M, N):
         raise ValueError("C has the wrong dtype or shape")
     lda, ldb, ldc = _rows_contiguous(A, "A"), _rows_contiguous(B, "B"), _rows_contiguous(C, "C")
@@ -309,7 +320,7 @@ def mlt_gemm(A: torch.Tensor, B: torch.Tensor, C: torch.Tensor | None = None, tr
     done = _fast.gemm(A, B, C, transB, stream)
     if done is not None:
         return done
-    M, N, K, lda, ldb, ldc, dt, C = _gemm_operands("mlt_gemm", A, B, C, transB)
+    M, N, K, lda, ldb, ldc, dt, C = _gemm_operands("mlt_gemm", A, B, C, transB, stream=stream)
     with _OtherDevice(A.device):
         rc = _lib.mlt_gemm(M, N, K, A.data_ptr(), lda, B.data_ptr(), ldb, int(transB),
                            C.data_ptr(), ldc, dt, _stream(stream, A.device))
@@ -339,7 +350,7 @@ TILING_AUTO, TILING_HORIZONTAL, TILING_VERTICAL, TILING_SQUARE = 0, 1, 2, 3
 def mlt_gemm_tiled(A: torch.Tensor, B: torch.Tensor, tiling: int, C: torch.Tensor | None = None,
                    transB: bool = False, stream=None) -> torch.Tensor:
     """mlt_gemm with the paper's tiling hint (TILING_AUTO / _HORIZONTAL / _VERTICAL / _SQUARE)."""
-    M, N, K, lda, ldb, ldc, dt, C = _gemm_operands("mlt_gemm_tiled", A, B, C, transB)
+    M, N, K, lda, ldb, ldc, dt, C = _gemm_operands("mlt_gemm_tiled", A, B, C, transB, stream=stream)
     with _OtherDevice(A.device):
         rc = _lib.mlt_gemm_tiled(M, N, K, A.data_ptr(), lda, B.data_ptr(), ldb, int(transB),
                                  C.data_ptr(), ldc, dt, int(tiling), _stream(stream, A.device))
@@ -356,7 +367,7 @@ def mlt_gemm_bias_act(A: torch.Tensor, B: torch.Tensor, bias: torch.Tensor | Non
     done = _fast.gemm_bias_act(A, B, bias, act, C, transB, stream)
     if done is not None:
         return done
-    M, N, K, lda, ldb, ldc, dt, C = _gemm_operands("mlt_gemm_bias_act", A, B, C, transB)
+    M, N, K, lda, ldb, ldc, dt, C = _gemm_operands("mlt_gemm_bias_act", A, B, C, transB, stream=stream)
     if bias is not None and (not bias.is_cuda or bias.dtype != A.dtype or tuple(bias.shape) != (N,)
                              or not bias.is_contiguous()):
         raise ValueError("bias must be a contiguous GPU tensor of N elements of the input dtype")
@@ -406,7 +417,7 @@ def mlt_mha_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, scale: float,
     if not (Q.is_contiguous() and K.is_contiguous() and V.is_contiguous()):
         raise ValueError("Q, K and V must be contiguous")
     if O is None:
-        O = torch.empty_like(Q)
+        O = _empty(Q.shape, Q.dtype, Q.device, stream)
     elif O.dtype != Q.dtype or O.shape != Q.shape or not O.is_contiguous():
         raise ValueError("O has the wrong dtype, shape or layout")
     with _OtherDevice(Q.device):
@@ -454,11 +465,11 @@ def mlt_quant_fp8(X: torch.Tensor, block_rows: int = 1, Xq: torch.Tensor | None 
     rows = int(block_rows)
     shape = (-(-K // 128), -(-M // rows) if rows > 0 else 0)
     if Xq is None:
-        Xq = torch.empty((M, -(-K // 16) * 16), dtype=E4M3, device=X.device)[:, :K]     # rows start on 16 bytes
+        Xq = _empty((M, -(-K // 16) * 16), E4M3, X.device, stream)[:, :K]               # rows start on 16 bytes
     elif Xq.dtype != E4M3 or Xq.shape != X.shape:
         raise ValueError("Xq must be a float8_e4m3fn tensor of X's shape")
     if S is None:
-        S = torch.empty(shape, dtype=torch.float32, device=X.device)
+        S = _empty(shape, torch.float32, X.device, stream)
     ldq, lds = _rows_contiguous(Xq, "Xq"), _scales(S, shape, "S")
     with _OtherDevice(X.device):
         rc = _lib.mlt_quant_fp8(M, K, X.data_ptr(), ldx, rows, Xq.data_ptr(), ldq, S.data_ptr(), lds, dt, _stream(stream, X.device))
@@ -485,7 +496,7 @@ def mlt_gemm_fp8(A: torch.Tensor, Sa: torch.Tensor, B: torch.Tensor, Sb: torch.T
     kb = -(-K // 128)
     ldsa, ldsb = _scales(Sa, (kb, M), "Sa"), _scales(Sb, (kb, -(-N // 128)), "Sb")
     if C is None:
-        C = torch.empty((M, N), dtype=dtype, device=A.device)
+        C = _empty((M, N), dtype, A.device, stream)
     elif tuple(C.shape) != (M, N):
         raise ValueError("C has the wrong shape")
     dt, ldc = _dtype_code(C), _rows_contiguous(C, "C")
@@ -522,7 +533,7 @@ def _append(name: str, Q, K, V, offsets, seq_lens, block_table, cos, sin, Kc, Vc
     if Q is not None:
         Hq, ldq = Q.shape[1] if Q.dim() == 3 else 0, _head_rows(Q, T, D, K.dtype, "Q")
         if Qo is None:
-            Qo = torch.empty((T, Hq, D), dtype=K.dtype, device=K.device)
+            Qo = _empty((T, Hq, D), K.dtype, K.device, stream)
         elif Qo.dtype != K.dtype or Qo.shape != Q.shape or not Qo.is_contiguous():
             raise ValueError("%s: Qo must be contiguous, of Q's shape and type" % name)
     elif Qo is not None:
@@ -608,7 +619,7 @@ def mlt_paged_attn_decode_fp8(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tenso
     if block_table.dim() != 2 or block_table.shape[0] != B or tuple(seq_lens.shape) != (B,):
         raise ValueError("%s: block_table / seq_lens shape" % name)
     if O is None:
-        O = torch.empty_like(Q, memory_format=torch.contiguous_format)
+        O = _empty(Q.shape, Q.dtype, Q.device, stream)
     elif O.dtype != Q.dtype or O.shape != Q.shape:
         raise ValueError("%s: O has the wrong dtype or shape" % name)
     for t in (Q, Kc, Vc, Ks, Vs, block_table, seq_lens, O):
