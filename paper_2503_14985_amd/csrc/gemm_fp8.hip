@@ -16,8 +16,8 @@
 // The 128-column tiles (gemm_fp8_kp_kernel) follow gemm_kp.hip: 256 to 128 rows x 128 columns, the two groups on alternate K steps, the scales in the LDS stage of their
 // step; K may be split in two parts, joined by the workgroup that comes last, or in up to 8, added by gemm_splitk_reduce_kernel. Which kernel runs is decided by estimated time (fp8_estimate).
 //
-// Measured: 8192 x 8192 x 8192 423 us, 2600 TFLOP/s; 777 x 4096 x 14336 61 us by 224 x 128 tiles
-// and two parts, 1490 TFLOP/s (bound by delivery: a CU takes 45 KB a step). A K step of a 256 x 256 tile, 1.98 us on random bits (1.65 on quantised N(0, 1)):
+// Measured: 8192 x 8192 x 8192 423 to 450 us by the board, 2440 to 2600 TFLOP/s (485 in a row of its own, at the power cap); 777 x 4096 x 14336 59 to 65 us by 224 x 128 tiles
+// and two parts, 1400 to 1540 TFLOP/s (its direct loads with barriers alone take 49 us, its MFMAs with barriers alone 48). A K step of a 256 x 256 tile, 1.98 us on random bits (1.65 on quantised N(0, 1)):
 // the MFMAs and barriers alone take 1.36, all but the direct loads 1.55, with sums by the MFMA itself (one scale for all of K) 1.76. It is 3250 clocks at the 1.8 GHz that the
 // board's power leaves: 2048 of the matrix units and as many of the LDS (192 KB of fragments read, 64 KB written, 128 bytes a clock).
 #include <stdio.h>
