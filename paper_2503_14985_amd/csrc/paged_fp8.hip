@@ -12,12 +12,12 @@
 //     dimension gets is free as long as Q's fragment agrees.
 //   * S^T leaves key 4 (l / 16) + r of query l % 16 in register r. Those are the k slots 8 (l / 16) .. + 7 of the second product
 //     (four from each half), so P needs no exchange between lanes, and the transposing LDS read fetches V for the same keys.
-// P and V are multiplied as fp16 whatever Q's type: e4m3 is exact in it. The scale of V goes into P: p = 2^(score - top) * (scale of V), `top` the running maximum of that
+// P and V are multiplied as fp16 whatever Q's type: e4m3 is exact in it. The scale of V goes into P: p = 2^(score - m - top) * (scale of V), m + top the running maximum of the
 // product's log2 over the wavefront's keys (it moves only when a product passes it by 8), so that a large scale on keys of little weight takes no bits from the
 // others. p is at most 2^8, 2^6 on top leaves it far from fp16's small end. It goes in as the sum of two fp16 numbers, itself rounded and what that left: 22 bits, as
 // good as fp32 beside the output's rounding, for 1 % of the time (64 sequences of up to 4096 keys 55.8 -> 56.4 us, one of 32768 17.0 -> 17.2; the matrix units are idle
-// for nine tenths of it), where one of 11 bits made fp16 results a third worse than an fp32 computation's. The weights' sum has a reference of its own, the maximum of the scores,
-// and is taken in fp32 before the rounding. A scale's exponent joins the score, its mantissa multiplies.
+// for nine tenths of it), where one of 11 bits made fp16 results a third worse than an fp32 computation's. The weights' sum is relative to m, the maximum of the scores,
+// and taken in fp32 before the rounding. A scale's exponent joins the score when m has been taken off (a large score would lose it), its mantissa multiplies.
 //
 // Keys are dealt in units to the 4 or 8 wavefronts of a workgroup and, with few (sequence, head) pairs, in ranges to several workgroups,
 // whose partial results (maximum, sum, outputs; fp32) are merged in a fixed order, by the one that comes last or by a second kernel.
@@ -181,8 +181,8 @@ __global__ __launch_bounds__(NW * 64, 4) void paged_fp8_kernel(PagedFp8 a) {
     }
   };
 
-  // log2 references: m of the weights (l), top of the weights times V's scales (o)
-  float m = -__builtin_inff(), l = 0.f, top = -__builtin_inff();
+  // log2 references: m of the weights (l), m + top of the weights times V's scales (o). mref: m, or 0 before it is known
+  float m = -__builtin_inff(), mref = 0.f, l = 0.f, top = 0.f;
   f32x4 o[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(NW * 64, 4) void paged_fp8_kernel(PagedFp8 a) {
       ks = *(const MLT_LDS float*)(uintptr_t)(side + 256 + lane * 4u);
       const float vs = *(const MLT_LDS float*)(uintptr_t)(side + 512 + lane * 4u);
       vm = __builtin_amdgcn_frexp_mantf(vs);
-      ve = (float)__builtin_amdgcn_frexp_expf(vs);
+      ve = vs == 0.f ? -150.f : (float)__builtin_amdgcn_frexp_expf(vs);    // (no scale is smaller)
     }
     u32x4 kr[2][KP];
 #pragma unroll
@@ -268,39 +268,38 @@ __global__ __launch_bounds__(NW * 64, 4) void paged_fp8_kernel(PagedFp8 a) {
         for (int r = 0; r < 4; ++r)
           if (u * PF_UNIT + p * 16 + 4 * g + r >= len) s[p][r] = -__builtin_inff();
     }
-    float mx = -__builtin_inff(), px = -__builtin_inff();
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const float four = __builtin_fmaxf(__builtin_fmaxf(s[p][0], s[p][1]), __builtin_fmaxf(s[p][2], s[p][3]));
-      mx = __builtin_fmaxf(mx, four);
-      px = __builtin_fmaxf(px, four + ves[p]);
-    }
-    if (__any(mx > m + PF_LAZY || px > top + PF_LAZY)) { // (-inf: the first time)
+    const float four[2] = {__builtin_fmaxf(__builtin_fmaxf(s[0][0], s[0][1]), __builtin_fmaxf(s[0][2], s[0][3])),
+                           __builtin_fmaxf(__builtin_fmaxf(s[1][0], s[1][1]), __builtin_fmaxf(s[1][2], s[1][3]))};
+    const float mx = __builtin_fmaxf(four[0], four[1]);
+    auto products = [&](float from) __attribute__((always_inline)) { return __builtin_fmaxf((four[0] - from) + ves[0], (four[1] - from) + ves[1]); };
+    if (__any(mx > m + PF_LAZY || products(mref) > top + PF_LAZY)) {       // (m = -inf: the first time)
       auto over_keys = [](float x) __attribute__((always_inline)) {
         x = __builtin_fmaxf(x, __shfl_xor(x, 16));
         return __builtin_fmaxf(x, __shfl_xor(x, 32));
       };
-      auto factor = [](float was, float now) __attribute__((always_inline)) { return now == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(was - now); };
-      const float m_was = m, top_was = top;
-      m = __builtin_fmaxf(m, over_keys(mx));
-      top = __builtin_fmaxf(top, over_keys(px));
-      l *= factor(m_was, m);
-      const float alpha = factor(top_was, top);
+      const float now = __builtin_fmaxf(m, over_keys(mx));
+      if (now > -__builtin_inff()) {                     // (else nothing has been added yet)
+        const float down = m - now, most = over_keys(products(now)), top_now = m == -__builtin_inff() ? most : __builtin_fmaxf(top + down, most);
+        const float alpha = __builtin_amdgcn_exp2f(down + (top - top_now));
+        l *= __builtin_amdgcn_exp2f(down);
+        m = mref = now;
+        top = top_now;
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[t][r] *= alpha;
+          for (int r = 0; r < 4; ++r) o[t][r] *= alpha;
+      }
     }
-    const float mref = m == -__builtin_inff() ? 0.f : m, tref = top == -__builtin_inff() ? 0.f : top;
     u32x4 pf, pl;                                        // P rounded, and what that left
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      const float up = ves[p] + PF_GAIN - tref;
+      const float up = ves[p] + (PF_GAIN - top);
       float e[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        l += __builtin_amdgcn_exp2f(s[p][r] - mref);
-        e[r] = __builtin_amdgcn_exp2f(s[p][r] + up) * vms[p];
+        const float d = s[p][r] - mref;
+        l += __builtin_amdgcn_exp2f(d);
+        e[r] = __builtin_amdgcn_exp2f(d + up) * vms[p];
       }
 #pragma unroll
       for (int r = 0; r < 4; r += 2) {
@@ -349,7 +348,7 @@ __global__ __launch_bounds__(NW * 64, 4) void paged_fp8_kernel(PagedFp8 a) {
       sm[wave * 16 + r16] = m;
       sl[wave * 16 + r16] = l;
     }
-    const float f = top == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(top - PF_GAIN - m);      // back to the weights' reference
+    const float f = __builtin_amdgcn_exp2f(top - PF_GAIN);                 // back to the weights' reference
     // register r of tile t is dimension 16 t + 4 g + r
 #pragma unroll
     for (int t = 0; t < NT; ++t)

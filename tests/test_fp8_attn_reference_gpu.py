@@ -98,3 +98,56 @@ def test_weights_keep_22_bits(lib, D, scale):
     err = (O.double() - o).abs()
     print("   worst %.2f of the tolerance, %.3f of the results beyond it" % (float((err / tol).max()), float((err > tol).double().mean())), flush=True)
     assert bool((tol < 1.5 * a.half_step(o, FP16)).all()) and bool((err <= tol).all())
+
+
+@pytest.mark.parametrize("split", [1, 3])
+@pytest.mark.parametrize("size", [1e3, 1e5, 1e7, 3e8, 1e20, -1e5, -3e8, -1e20])
+def test_scores_of_any_size(lib, key_split, size, split):
+    """Equal scores, however large, weigh all keys alike: the mean of the values, whose scales differ. And with one key in front by any margin it is that key's value."""
+    g = torch.Generator().manual_seed(23)
+    H, D, block, n = 2, 64, 32, 1600
+    nb = n // block
+    q = torch.ones((1, 2 * H, D), dtype=BF16)
+    kc = torch.ones((nb, H, block, D)).to(a.F8)
+    vc = (torch.rand((nb, H, block, D), generator=g) * 200 + 100).to(a.F8)
+    ks, vs = torch.ones((nb, H)), torch.exp2(torch.rand((nb, H), generator=g) * 12 - 12)
+    c = on_gpu(dict(q=q, kc=kc, vc=vc, ks=ks, vs=vs, table=torch.randperm(nb, generator=g).to(torch.int32).reshape(1, -1).contiguous(),
+                    lens=torch.tensor([n - 3], dtype=torch.int32), scale=size / D))
+    key_split(split)
+    O = run(lib, c).double()
+    o, more = a.exact(**c)
+    # fp32 sums over n keys, exp2 and the references' rescalings (sizes of at most 16 here, whatever the scores': the same number is taken off them first)
+    rel = 2.0 ** -8 + 2.0 ** -22 + 2 * (n * 2.0 ** -24 + 8 * 16 * 3 * 2.0 ** -24)
+    assert bool(((O - o).abs() <= rel * o.abs()).all()), float(((O - o).abs() / o.abs()).max())
+    if size > 0:
+        first = int(c["table"][0, 7])
+        c["kc"].view(torch.uint8)[first, :, 5] = 0x40                      # 2.0: twice the others' score
+        O = run(lib, c).double()
+        want = (c["vc"][first, :, 5].double() * c["vs"][first].double()[:, None]).repeat_interleave(2, 0)
+        assert bool(((O[0] - want).abs() <= rel * want).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_zero_scales(lib, key_split, dtype):
+    """Blocks whose values' scale is 0 (a quantiser's for a block of zeros) count as zeros and take no bits from the others, whose scales are small."""
+    g = torch.Generator().manual_seed(29)
+    H, D, block, n = 2, 128, 32, 2048
+    nb = n // block
+    vs = torch.exp2(torch.rand((nb, H), generator=g) - 12)
+    q = torch.randn((1, 2 * H, D), generator=g).to(dtype)
+    kc, vc = (torch.rand((nb, H, block, D), generator=g).mul(200).add(100).to(a.F8) for _ in range(2))
+    table = torch.arange(nb, dtype=torch.int32).reshape(1, -1)
+    key_split(1)
+    c = on_gpu(dict(q=q, kc=kc, vc=vc, ks=torch.full((nb, H), 2.0 ** -12), vs=vs, table=table, lens=torch.tensor([n], dtype=torch.int32), scale=1 / D ** 0.5))
+    for lo in (1.0, 2.0 ** -30, 2.0 ** -60):
+        small = c["vs"] * lo
+        none = small.clone()
+        none[::3] = 0.0
+        unit = 1.0 if lo == 1.0 else 1 / lo                                # (compared in units of the scales: the outputs themselves are small)
+        O = run(lib, dict(c, vs=none)).double() * unit
+        ref = dict(c, vs=c["vs"].clone())
+        ref["vs"][::3] = 2.0 ** -100
+        o, more = a.exact(**ref)
+        tol = a.tolerance(o, more, n, D, dtype, 8, WEIGHT_HALF) + (2.0 ** -25 * unit if dtype == FP16 else 0.0)
+        if dtype == BF16 or lo == 1.0:
+            assert bool(((O - o).abs() <= tol).all()), (lo, float(((O - o).abs() / tol).max()))
