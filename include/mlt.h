@@ -181,7 +181,8 @@ int mlt_paged_attn_decode(int64_t B, int64_t H, int64_t D, int64_t block_size, i
  * e4m3 is the OCP format (1 sign, 4 exponent and 3 mantissa bits, largest value 448, NaN but no infinities), one byte an
  * element. A number is its e4m3 value times the fp32 scale of its block. The scales that the library writes are powers of
  * two: the smallest s >= 2^-100 with max |x| <= 448 s over the block's finite x, so that the rounding to e4m3 (to nearest, ties to
- * even) is the only one. Infinities and NaN become NaN. The scales that it reads may be any numbers from 2^-100 to 2^126.
+ * even) is the only one. Infinities and NaN become NaN. The scales that it reads may be any numbers from 2^-100 to 2^126,
+ * and 0 for a block that counts as zeros.
  */
 
 /*

@@ -81,3 +81,20 @@ def test_prefill_rows_without_a_place(lib):
         return t
     for fp8 in (False, True):
         append_case(lib, [1900, 200], [0, 4], 16, 2, 128, 16, 128, False, BF16, fp8, 29, tables=bad, positions=700)
+
+
+def test_zero_scale_of_earlier_tokens(lib):
+    """Earlier tokens with a scale of 0 are zeros, and stay so in the scale of the new ones."""
+    H, D, block = 2, 64, 16
+    kc = torch.full((1, H, block, D), 3.0).to(F8).to(dev())
+    vc, ks, vs = kc.clone(), torch.zeros((1, H), device=dev()), torch.zeros((1, H), device=dev())
+    k = torch.randn((2, H, D), generator=torch.Generator().manual_seed(5)).to(BF16).to(dev())
+    k[:, 1] = 0.0                                                          # a head whose new tokens are zeros too
+    at = [torch.tensor(v, dtype=torch.int32, device=dev()) for v in ([0, 2], [11], [[0]])]
+    lib.mlt_paged_append_fp8(None, k, k, *at, None, None, kc, vc, ks, vs)
+    for c, s in ((kc, ks), (vc, vs)):
+        back = f64(c) * f64(s)[..., None, None]
+        assert (back[0, :, :9] == 0).all()
+        want, scales = u.append_fp8(f64(k), np.zeros((1, H, block, D)), np.full((1, H), 2.0 ** -100), [(0, 0, 9, 0, 9), (1, 0, 10, 0, 10)])
+        assert np.array_equal(f64(s), scales) and np.array_equal(f64(c)[0, :, 9:11], want[0, :, 9:11])
+        assert (f64(c)[0, :, 11:] == 3.0).all()

@@ -78,3 +78,18 @@ def test_thirteen_bits_below_the_largest_product(variant):
         got = product(a.to(u.F8), b.to(u.F8), N, torch.float16)
         off = np.abs(got - 7 * value)
         assert (off == 0).all() if exact else (off < 7 * 8.0).all(), (value, got[:4])
+
+
+@pytest.mark.parametrize("variant", KERNELS, indirect=True)
+def test_zero_scales(variant):
+    """Blocks of A or B with a scale of 0 add nothing, whatever their numbers."""
+    from paper_2503_14985_amd import binding
+    dev, (M, N, K) = torch.device("cuda:0"), (150, 300, 512)
+    g = torch.Generator().manual_seed(7)
+    a, b = (torch.randint(-8, 9, (r, K), generator=g).float() for r in (M, N))
+    sa, sb = torch.exp2(torch.randint(-2, 3, (4, M), generator=g).float()), torch.exp2(torch.randint(-2, 3, (4, 3), generator=g).float())
+    sa[1, ::2], sb[2, 1] = 0.0, 0.0
+    ref = ((a.double() * sa.t().double().repeat_interleave(128, 1)) @ (b.double() * sb.t().double().repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)).t())
+    C = binding.mlt_gemm_fp8(a.to(u.F8).to(dev), sa.to(dev), b.to(u.F8).to(dev), sb.to(dev), dtype=torch.bfloat16)
+    # whole numbers of at most 64 to a product: exact in a group's 13 bits and in fp32 but for the smallest scales' 2^-4; then the output's rounding
+    assert torch.equal(C.double().cpu(), ref.float().to(torch.bfloat16).double())
