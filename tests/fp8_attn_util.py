@@ -111,30 +111,34 @@ def emulate(q, k, ks, v, vs, scale, waves, n, wrong=""):
     """The kernel's way for one query: q [D], k, v [units, 32, D], ks, vs [units]. wrong: a mistake to make."""
     parts = []
     for w in range(waves):
-        m = top = -math.inf
+        m, top = np.float32(-math.inf), np.float32(0)                    # top is relative to m
         l, o = 0.0, np.zeros(q.shape[0])
         for u in range(w, k.shape[0], waves):
             mant, ex = np.frexp(vs[u])
-            s = (k[u] @ q) * (ks[u] * scale * LOG2E)
+            if wrong == "scale reference":                               # P against the largest value scale met, whatever its keys weigh
+                ex = 0
+            s = np.float32((k[u] @ q) * (ks[u] * scale * LOG2E))
             s[np.arange(32) + 32 * u >= n] = -math.inf
             mx = s.max()
-            px = mx + (0 if wrong == "scale reference" else ex)          # (that mistake: P against the largest value scale met, whatever its keys weigh)
-            if mx > m + LAZY or px > top + LAZY:
-                m_was, top_was, m, top = m, top, max(m, mx), max(top, px)
+            if mx > m + LAZY or mx - m + ex > top + LAZY:
+                now = max(m, mx)
+                down, most = m - now, np.float32(mx - now + ex)
+                top_now = max(top + down, most) if m > -math.inf else most
                 if wrong != "sum kept":
-                    l *= 2.0 ** (m_was - m) if m > -math.inf else 1
+                    l *= 2.0 ** down
                 if wrong != "outputs kept":
-                    o *= 2.0 ** (top_was - top) if top > -math.inf else 1
+                    o *= 2.0 ** (down + (top - top_now))
+                m, top = now, top_now
             if wrong == "scale reference":
                 big = np.maximum.accumulate(vs[w:u + 1:waves])
                 if len(big) > 1:
                     o *= big[-2] / big[-1]
-                o = o + np.float16(2.0 ** (s - top + GAIN) * (vs[u] / big[-1])).astype(float) @ v[u]
+                o = o + np.float16(2.0 ** (s - m - top + GAIN) * (vs[u] / big[-1])).astype(float) @ v[u]
             else:
-                o = o + two_halves(2.0 ** (s + ex + GAIN - top) * mant) @ v[u]
-            l += (2.0 ** (s - m)).sum()
+                o = o + two_halves(2.0 ** np.float64(s - m + np.float32(ex + (GAIN - top))) * mant) @ v[u]
+            l += (2.0 ** np.float64(s - m)).sum()
         last = np.max(vs[w::waves]) if wrong == "scale reference" else 1.0
-        parts.append((m, l, o * last * 2.0 ** (top - GAIN - m) if m > -math.inf else o))
+        parts.append((float(m), l, o * last * 2.0 ** (float(top) - GAIN)))
     M = max(p[0] for p in parts)
     L = sum(p[1] * 2.0 ** (p[0] - M) for p in parts)
     return sum(p[2] * 2.0 ** (p[0] - M) for p in parts) / L
