@@ -275,6 +275,84 @@ int mlt_paged_attn_decode_fp8(int64_t B, int64_t Hq, int64_t H, int64_t D, int64
                               int64_t num_blocks, const void* Q, const void* Kc, const void* Vc, const float* Ks, const float* Vs,
                               const int32_t* block_table, const int32_t* seq_lens, void* O, float scale, int dtype, void* stream);
 
+/*
+ * ---- Prompts, shared prefixes, 4-bit weights.
+ */
+
+/*
+ * Attention forward of a batch of sequences of different lengths, packed one after the other, with Hq / H query heads to each key/value head
+ * (query head q reads head q / (Hq / H)). For query i of the n of sequence b, over its m keys:
+ *   o = sum_j softmax_j(scale * q . k_j) v_j,   j < m, with `causal` != 0 only j <= m - n + i
+ * (the last query sees all keys: with n == m the lower triangle, with n < m the queries are the sequence's last tokens). A query that sees no key
+ * (m == 0, or m < n) gives zeros.
+ *   Q, K, V      device, `dtype`: Tq rows of Hq and Tk rows of H heads of D elements side by side, row strides ldq, ldk, ldv (elements, multiples of
+ *                8: parts of one fused projection's result are fine)
+ *   q_offsets    device, int32 [B + 1], 0 <= q_offsets[0] <= ... <= q_offsets[B] <= Tq: rows q_offsets[b] .. q_offsets[b + 1] - 1 of Q and O are
+ *                sequence b's queries (none, one, many)
+ *   k_offsets    device, int32 [B + 1], the same for its keys, up to Tk; may be q_offsets
+ *   O            device, `dtype`: Tq rows of Hq heads, row stride ldo. Rows of no sequence are neither read nor written.
+ * Weights are rounded to `dtype` before they multiply V, relative to a maximum of their row; their sum is that of the rounded ones. What a query does not see
+ * has no influence on it, whatever it holds (infinities and NaN too). Offsets out of their range or order give wrong results for their sequences, but no access out
+ * of range. D must be 64 or 128, ldq, ldk, ldv, ldo multiples of 8 (MLT_ERR_UNSUPPORTED); all tensors of `dtype` 16-byte aligned, scale finite,
+ * H a divisor of Hq (MLT_ERR_INVALID_ARG). Tq, B or Hq equal to 0 is a no-op.
+ */
+int mlt_mha_packed_fwd(int64_t Tq, int64_t Tk, int64_t B, int64_t Hq, int64_t H, int64_t D, const void* Q, int64_t ldq, const void* K, int64_t ldk,
+                       const void* V, int64_t ldv, const int32_t* q_offsets, const int32_t* k_offsets, void* O, int64_t ldo, float scale,
+                       int causal, int dtype, void* stream);
+
+/*
+ * mlt_mha_packed_fwd with `causal`, for new tokens whose keys and values are in the paged cache already (mlt_paged_append puts them there):
+ *   Q, ldq, O, ldo            as there, T rows
+ *   offsets                   device, int32 [B + 1]: the rows of each sequence, as for mlt_paged_append
+ *   seq_lens, block_table, Kc, Vc, block_size, max_blocks, num_blocks   as for mlt_paged_append: seq_lens[b] counts the sequence's tokens WITH the
+ *                             new ones. The i-th of its n new tokens has position seq_lens[b] - n + i and sees the keys up to there.
+ * A position below 0 gives zeros. Only slots below seq_lens[b] are read. Lengths are clamped to 0 .. max_blocks * block_size, block numbers to 0 .. num_blocks - 1 (wrong result
+ * for that sequence, no access out of range). Requirements as for mlt_mha_packed_fwd; block_size a multiple of 16 up to 1024.
+ */
+int mlt_paged_attn_prompt(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks, int64_t num_blocks,
+                          const void* Q, int64_t ldq, const void* Kc, const void* Vc, const int32_t* offsets, const int32_t* seq_lens,
+                          const int32_t* block_table, void* O, int64_t ldo, float scale, int dtype, void* stream);
+
+/*
+ * mlt_paged_attn_decode for a batch whose sequences begin with the same prefix_len tokens, with Hq / H query heads to each key/value head. The prefix's
+ * keys and values are read once for all sequences:
+ *   o = sum_j softmax_j(scale * q . k_j) v_j,   j = 0 .. seq_lens[b] - 1,   0 <= seq_lens[b] <= max_blocks * block_size
+ *   Q, O           device, contiguous [B, Hq, D]
+ *   Kc, Vc, block_size, max_blocks, num_blocks   as for mlt_paged_attn_decode
+ *   prefix_table   device, int32 [ceil(prefix_len / block_size)]: the blocks of key 0 .. prefix_len - 1 (may be a row of block_table). prefix_len on the host; 0 for none
+ *                  (prefix_table unused)
+ *   block_table    device, int32 [B, max_blocks], as for mlt_paged_append: key j >= prefix_len of sequence b is in block block_table[b][j / block_size].
+ *                  Entries below prefix_len / block_size are not read.
+ *   seq_lens       device, int32 [B]: all of a sequence's tokens, the prefix's among them. A sequence may end inside the prefix; one without keys gives zeros.
+ *   work           device, 16-byte aligned, work_bytes long: fp32 partial results, needed only while the call runs; or NULL: the library's scratch of the stream. With less than
+ *                  mlt_paged_attn_decode_prefix_work says, or NULL on a stream that records into a graph, the prefix is read again for
+ *                  every sequence. Two captured graphs that may run at the same time need a work of their own each.
+ * Weights keep about 16 bits or more whatever `dtype`. The limits of what is read, clamping and requirements are those of mlt_paged_attn_decode_fp8;
+ * prefix_len must lie in 0 .. max_blocks * block_size (MLT_ERR_INVALID_ARG).
+ */
+int mlt_paged_attn_decode_prefix(int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks, int64_t num_blocks,
+                                 const void* Q, const void* Kc, const void* Vc, const int32_t* prefix_table, int64_t prefix_len,
+                                 const int32_t* block_table, const int32_t* seq_lens, void* O, float scale, void* work, int64_t work_bytes,
+                                 int dtype, void* stream);
+
+/* Bytes of `work` for a call of these sizes on the current device (0: the call needs none), or a negative mlt_status. */
+int64_t mlt_paged_attn_decode_prefix_work(int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks, int64_t prefix_len);
+
+/*
+ * Few rows times a matrix of 4-bit weights: C = A * W^T, W[n][k] = S[k / group][n] * (q[n][k] - z),
+ *   A       device, M x K row-major of `dtype`, row stride lda >= K
+ *   Wq      device, N rows of K / 2 bytes, row stride ldw >= K / 2 bytes: q[n][k], 0 .. 15, is the low half of byte k / 2 of row n for even k, the high half for odd k
+ *   S       device, `dtype` [ceil(K / group)][N], row stride lds >= N
+ *   Z       device, uint8 [ceil(K / group)][N], row stride ldz >= N: z, 0 .. 15; or NULL: z = 8 (ldz unused)
+ *   C       device, M x N row-major of `dtype`, row stride ldc >= N; written, never read
+ * group is 32, 64 or 128; the last one of a row may be shorter. Products and the sum over a group are fp32, as is the sum over the groups, each times its scale; C is
+ * rounded once. An infinity in a row of A may give NaN. The order of the sums goes by the sizes; equal calls give equal bits. K a multiple of 32, lda a multiple of 8,
+ * ldw of 16 (MLT_ERR_UNSUPPORTED); A and Wq 16-byte, S and C 2-byte aligned. Any M is taken; the kernel is made for up to 64 rows (the weights are read again for
+ * every 64). M == 0 or N == 0 is a no-op, K == 0 stores zeros.
+ */
+int mlt_gemm_w4(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const void* Wq, int64_t ldw, int64_t group, const void* S, int64_t lds,
+                const uint8_t* Z, int64_t ldz, void* C, int64_t ldc, int dtype, void* stream);
+
 /* Static, human-readable text for a status code. */
 const char* mlt_status_string(int status);
 

@@ -22,7 +22,8 @@ MLT_ERR_SCRATCH = -5
 # include/mlt.h (the operations) and include/mlt_diag.h (probes, timing hooks, kernel-choice overrides)
 EXPORTS = ("mlt_gemm", "mlt_gemm_noalloc", "mlt_gemm_acc", "mlt_gemm_tiled", "mlt_gemm_bias_act", "mlt_mha_fwd",
            "mlt_paged_attn_decode", "mlt_quant_fp8", "mlt_gemm_fp8", "mlt_paged_append", "mlt_paged_append_fp8",
-           "mlt_paged_attn_decode_fp8", "mlt_status_string", "mlt_version")
+           "mlt_paged_attn_decode_fp8", "mlt_mha_packed_fwd", "mlt_paged_attn_prompt", "mlt_paged_attn_decode_prefix",
+           "mlt_paged_attn_decode_prefix_work", "mlt_gemm_w4", "mlt_status_string", "mlt_version")
 DIAG_EXPORTS = ("mlt_probe_mfma", "mlt_probe_mfma16", "mlt_probe_hbm_read", "mlt_set_timing_events",
                 "mlt_last_kernel", "mlt_query_tiling", "mlt_diag_force_variant",
                 "mlt_diag_force_k_parts", "mlt_diag_force_key_split", "mlt_diag_set_persistent_grid")
@@ -64,6 +65,16 @@ _lib.mlt_paged_append_fp8.restype = _i32
 _lib.mlt_paged_append_fp8.argtypes = [_i64] * 8 + [_p, _i64] * 3 + [_p] * 5 + [_i64, _i64, _i32, _p, _p, _p, _p, _p, _i32, _p]
 _lib.mlt_paged_attn_decode_fp8.restype = _i32
 _lib.mlt_paged_attn_decode_fp8.argtypes = [_i64] * 7 + [_p] * 8 + [ctypes.c_float, _i32, _p]
+_lib.mlt_mha_packed_fwd.restype = _i32
+_lib.mlt_mha_packed_fwd.argtypes = [_i64] * 6 + [_p, _i64] * 3 + [_p, _p, _p, _i64, ctypes.c_float, _i32, _i32, _p]
+_lib.mlt_paged_attn_prompt.restype = _i32
+_lib.mlt_paged_attn_prompt.argtypes = [_i64] * 8 + [_p, _i64] + [_p] * 6 + [_i64, ctypes.c_float, _i32, _p]
+_lib.mlt_paged_attn_decode_prefix.restype = _i32
+_lib.mlt_paged_attn_decode_prefix.argtypes = [_i64] * 7 + [_p] * 4 + [_i64] + [_p] * 3 + [ctypes.c_float, _p, _i64, _i32, _p]
+_lib.mlt_paged_attn_decode_prefix_work.restype = _i64
+_lib.mlt_paged_attn_decode_prefix_work.argtypes = [_i64] * 7
+_lib.mlt_gemm_w4.restype = _i32
+_lib.mlt_gemm_w4.argtypes = [_i64, _i64, _i64, _p, _i64, _p, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _i32, _p]
 _lib.mlt_probe_mfma.restype = _i32
 _lib.mlt_probe_mfma.argtypes = [_i32, _p, _p, ctypes.POINTER(ctypes.c_double), _p]
 _lib.mlt_probe_mfma16.restype = _i32
@@ -632,3 +643,163 @@ def mlt_paged_attn_decode_fp8(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tenso
     if rc != MLT_OK:
         raise MltError(rc, name)
     return O
+
+
+# ---- prompts, shared prefixes, 4-bit weights
+
+def _offsets(name: str, t: torch.Tensor, B: int, what: str) -> None:
+    if t.dtype != torch.int32 or tuple(t.shape) != (B + 1,) or not t.is_contiguous():
+        raise ValueError("%s: %s must be a contiguous int32 tensor of %d elements" % (name, what, B + 1))
+
+
+def _packed_queries(name: str, Q: torch.Tensor, O, stream):
+    """dtype code, row strides and output (allocated when None) of packed queries [T, Hq, D]."""
+    if Q.dim() != 3:
+        raise ValueError("%s: Q must be [tokens, heads, D]" % name)
+    T, Hq, D = Q.shape
+    dt, ldq = _dtype_code(Q), _head_rows(Q, T, D, Q.dtype, "Q")
+    if O is None:
+        O = _empty(Q.shape, Q.dtype, Q.device, stream)
+    elif O.shape != Q.shape:
+        raise ValueError("%s: O has the wrong shape" % name)
+    return dt, ldq, _head_rows(O, T, D, Q.dtype, "O"), O
+
+
+def _paged_cache(name: str, Kc: torch.Tensor, Vc: torch.Tensor, D: int, dtype) -> None:
+    if Kc.dim() != 4 or Vc.shape != Kc.shape or Kc.shape[3] != D:
+        raise ValueError("%s: cache shape does not match Q" % name)
+    if Kc.dtype != dtype or Vc.dtype != dtype:
+        raise TypeError("%s: the cache must be of Q's type" % name)
+    if not Kc.is_contiguous() or not Vc.is_contiguous():
+        raise ValueError("%s: the cache must be contiguous" % name)
+
+
+def _paged_tables(name: str, block_table: torch.Tensor, seq_lens: torch.Tensor) -> int:
+    if block_table.dtype != torch.int32 or seq_lens.dtype != torch.int32:
+        raise ValueError("%s: block_table and seq_lens must be int32" % name)
+    if block_table.dim() != 2 or seq_lens.dim() != 1 or block_table.shape[0] != seq_lens.shape[0]:
+        raise ValueError("%s: block_table / seq_lens shape" % name)
+    if not block_table.is_contiguous() or not seq_lens.is_contiguous():
+        raise ValueError("%s: block_table and seq_lens must be contiguous" % name)
+    return seq_lens.shape[0]
+
+
+def mlt_mha_packed_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, q_offsets: torch.Tensor, k_offsets: torch.Tensor | None, scale: float,
+                       causal: bool = True, O: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Attention of packed sequences. Q [Tq, Hq, D], K, V [Tk, H, D] with Hq a multiple of H: a token's heads side by side, any row stride; q_offsets
+    (k_offsets; None: the same) int32 [B + 1]: the rows of each sequence. causal: the last query of a sequence sees all its keys, the one before one
+    less. Returns O [Tq, Hq, D]; rows of no sequence are left as they are."""
+    name = "mlt_mha_packed_fwd"
+    if k_offsets is None:
+        k_offsets = q_offsets
+    _gpu(name, Q, K, V, q_offsets, k_offsets, O)
+    dt, ldq, ldo, O = _packed_queries(name, Q, O, stream)
+    T, Hq, D = Q.shape
+    if K.dim() != 3 or V.shape != K.shape:
+        raise ValueError("%s: K and V must be [tokens, heads, D] of one shape" % name)
+    Tk, H = K.shape[:2]
+    ldk, ldv = _head_rows(K, Tk, D, Q.dtype, "K"), _head_rows(V, Tk, D, Q.dtype, "V")
+    B = q_offsets.numel() - 1
+    _offsets(name, q_offsets, B, "q_offsets")
+    _offsets(name, k_offsets, B, "k_offsets")
+    with _OtherDevice(Q.device):
+        rc = _lib.mlt_mha_packed_fwd(T, Tk, B, Hq, H, D, Q.data_ptr(), ldq, K.data_ptr(), ldk, V.data_ptr(), ldv, q_offsets.data_ptr(), k_offsets.data_ptr(),
+                                     O.data_ptr(), ldo, float(scale), int(bool(causal)), dt, _stream(stream, Q.device))
+    if rc != MLT_OK:
+        raise MltError(rc, name)
+    return O
+
+
+def mlt_paged_attn_prompt(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, offsets: torch.Tensor, seq_lens: torch.Tensor, block_table: torch.Tensor,
+                          scale: float, O: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Causal attention of the new tokens of sequences whose keys are in the paged cache (see mlt_paged_append). Q [T, Hq, D]; Kc, Vc [num_blocks, H,
+    block_size, D] with Hq a multiple of H; offsets int32 [B + 1]: the rows of each sequence; seq_lens int32 [B]: its tokens with the new ones;
+    block_table int32 [B, max_blocks]. Returns O [T, Hq, D]; rows of no sequence are left as they are."""
+    name = "mlt_paged_attn_prompt"
+    _gpu(name, Q, Kc, Vc, offsets, seq_lens, block_table, O)
+    dt, ldq, ldo, O = _packed_queries(name, Q, O, stream)
+    T, Hq, D = Q.shape
+    _paged_cache(name, Kc, Vc, D, Q.dtype)
+    B = _paged_tables(name, block_table, seq_lens)
+    _offsets(name, offsets, B, "offsets")
+    nb, H, bs, _ = Kc.shape
+    with _OtherDevice(Q.device):
+        rc = _lib.mlt_paged_attn_prompt(T, B, Hq, H, D, bs, block_table.shape[1], nb, Q.data_ptr(), ldq, Kc.data_ptr(), Vc.data_ptr(), offsets.data_ptr(),
+                                        seq_lens.data_ptr(), block_table.data_ptr(), O.data_ptr(), ldo, float(scale), dt, _stream(stream, Q.device))
+    if rc != MLT_OK:
+        raise MltError(rc, name)
+    return O
+
+
+def mlt_paged_attn_decode_prefix_work(B: int, Hq: int, H: int, D: int, block_size: int, max_blocks: int, prefix_len: int) -> int:
+    """Bytes of `work` for a call of these sizes on the current GPU."""
+    n = _lib.mlt_paged_attn_decode_prefix_work(B, Hq, H, D, block_size, max_blocks, prefix_len)
+    if n < 0:
+        raise MltError(n, "mlt_paged_attn_decode_prefix_work")
+    return n
+
+
+def mlt_paged_attn_decode_prefix(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, prefix_table: torch.Tensor | None, prefix_len: int,
+                                 block_table: torch.Tensor, seq_lens: torch.Tensor, scale: float, O: torch.Tensor | None = None,
+                                 work: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """One query a sequence over a prefix that all share, read once, and its own keys. Q [B, Hq, D]; Kc, Vc [num_blocks, H, block_size, D] with Hq a
+    multiple of H; prefix_table int32 [at least ceil(prefix_len / block_size)]: the prefix's blocks; block_table int32 [B, max_blocks] and seq_lens int32 [B]: as for
+    mlt_paged_append, the prefix's tokens among a sequence's. work: uint8, mlt_paged_attn_decode_prefix_work bytes, for calls that are captured into
+    a graph. Returns O [B, Hq, D]."""
+    name = "mlt_paged_attn_decode_prefix"
+    _gpu(name, Q, Kc, Vc, prefix_table, block_table, seq_lens, O, work)
+    dt, P = _dtype_code(Q), int(prefix_len)
+    if Q.dim() != 3:
+        raise ValueError("%s: Q must be [sequences, heads, D]" % name)
+    Bq, Hq, D = Q.shape
+    _paged_cache(name, Kc, Vc, D, Q.dtype)
+    B = _paged_tables(name, block_table, seq_lens)
+    if B != Bq:
+        raise ValueError("%s: block_table / seq_lens shape" % name)
+    nb, H, bs, _ = Kc.shape
+    if P > 0 and (prefix_table is None or prefix_table.dtype != torch.int32 or prefix_table.dim() != 1 or not prefix_table.is_contiguous()
+                  or prefix_table.shape[0] * bs < P):
+        raise ValueError("%s: prefix_table must be a contiguous int32 tensor with a block for every %d keys of the prefix" % (name, bs))
+    if O is None:
+        O = _empty(Q.shape, Q.dtype, Q.device, stream)
+    elif O.dtype != Q.dtype or O.shape != Q.shape:
+        raise ValueError("%s: O has the wrong dtype or shape" % name)
+    if not Q.is_contiguous() or not O.is_contiguous():
+        raise ValueError("%s: Q and O must be contiguous" % name)
+    if work is not None and (work.dtype != torch.uint8 or not work.is_contiguous()):
+        raise ValueError("%s: work must be a contiguous uint8 tensor" % name)
+    with _OtherDevice(Q.device):
+        rc = _lib.mlt_paged_attn_decode_prefix(B, Hq, H, D, bs, block_table.shape[1], nb, Q.data_ptr(), Kc.data_ptr(), Vc.data_ptr(),
+                                               None if prefix_table is None else prefix_table.data_ptr(), P, block_table.data_ptr(), seq_lens.data_ptr(),
+                                               O.data_ptr(), float(scale), None if work is None else work.data_ptr(), 0 if work is None else work.numel(),
+                                               dt, _stream(stream, Q.device))
+    if rc != MLT_OK:
+        raise MltError(rc, name)
+    return O
+
+
+def mlt_gemm_w4(A: torch.Tensor, Wq: torch.Tensor, S: torch.Tensor, Z: torch.Tensor | None = None, group: int = 128, C: torch.Tensor | None = None,
+                stream=None) -> torch.Tensor:
+    """C = A @ W.T with 4-bit weights: A [M, K]; Wq uint8 [N, K / 2], element k in the low (even k) or high half of byte k / 2; S [ceil(K / group), N] of
+    A's type; Z uint8 [ceil(K / group), N] or None (8): W[n, k] = S[k // group, n] * (q[n, k] - Z[k // group, n]). Returns C [M, N]."""
+    name = "mlt_gemm_w4"
+    _gpu(name, A, Wq, S, Z, C)
+    dt, g = _dtype_code(A), int(group)
+    if Wq.dtype != torch.uint8 or (Z is not None and Z.dtype != torch.uint8) or S.dtype != A.dtype:
+        raise TypeError("%s: Wq and Z must be uint8 tensors, S of A's type" % name)
+    lda, ldw, lds = _rows_contiguous(A, "A"), _rows_contiguous(Wq, "Wq"), _rows_contiguous(S, "S")
+    M, K = A.shape
+    N = Wq.shape[0]
+    shape = (-(-K // g) if g > 0 else 0, N)
+    if 2 * Wq.shape[1] != K or (g > 0 and tuple(S.shape) != shape) or (Z is not None and Z.shape != S.shape):
+        raise ValueError("%s: Wq must be [N, K / 2], S and Z [ceil(K / group), N]" % name)
+    if C is None:
+        C = _empty((M, N), A.dtype, A.device, stream)
+    elif C.dtype != A.dtype or tuple(C.shape) != (M, N):
+        raise ValueError("%s: C has the wrong dtype or shape" % name)
+    with _OtherDevice(A.device):
+        rc = _lib.mlt_gemm_w4(M, N, K, A.data_ptr(), lda, Wq.data_ptr(), ldw, g, S.data_ptr(), lds, None if Z is None else Z.data_ptr(),
+                              0 if Z is None else _rows_contiguous(Z, "Z"), C.data_ptr(), _rows_contiguous(C, "C"), dt, _stream(stream, A.device))
+    if rc != MLT_OK:
+        raise MltError(rc, name)
+    return C

@@ -1,0 +1,53 @@
+// One query row over keys 0 .. end - 1 by one wavefront: 64 keys at a time, a lane's score each, the running maximum and sum of a softmax, then the
+// values' rows with the lanes along the head's elements.
+#pragma once
+
+#include "mlt_common.h"
+
+namespace mlt {
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) x = __builtin_fmaxf(x, __shfl_xor(x, s));
+  return x;
+}
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) x += __shfl_xor(x, s);
+  return x;
+}
+
+// krow(j), vrow(j): first element of key (value) j in K (V)
+template <typename Tag, int D, typename KRow, typename VRow>
+__device__ __forceinline__ void attend_row(const uint16_t* q, uint16_t* out, int64_t end, const uint16_t* K, const uint16_t* V, KRow krow, VRow vrow, float c) {
+  constexpr int E = D / 64;
+  const int lane = threadIdx.x & 63;
+  float m = -__builtin_inff(), l = 0.f, o[E] = {};
+  for (int64_t j0 = 0; j0 < end; j0 += 64) {
+    const int64_t j = j0 + lane;
+    float s = -__builtin_inff();
+    if (j < end) {
+      const uint16_t* k = K + krow(j);
+      s = 0.f;
+      for (int d = 0; d < D; ++d) s = __builtin_fmaf(Elem<Tag>::to_f32(q[d]), Elem<Tag>::to_f32(k[d]), s);
+      s *= c;
+    }
+    const float top = __builtin_fmaxf(m, wave_max(s)), ref = top == -__builtin_inff() ? 0.f : top;
+    const float alpha = __builtin_amdgcn_exp2f(m - ref), p = __builtin_amdgcn_exp2f(s - ref);
+    l = l * alpha + wave_sum(p);
+    m = top;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= alpha;
+    const int n = end - j0 < 64 ? (int)(end - j0) : 64;
+    for (int i = 0; i < n; ++i) {
+      const uint16_t* v = V + vrow(j0 + i);
+      const float w = __shfl(p, i);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(w, Elem<Tag>::to_f32(v[e * 64 + lane]), o[e]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) out[e * 64 + lane] = Elem<Tag>::from_f32(end > 0 ? o[e] / l : 0.f);
+}
+
+}  // namespace mlt

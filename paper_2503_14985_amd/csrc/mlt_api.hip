@@ -144,6 +144,56 @@ struct TimedRegion {
 
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+void note_name(const char (&name)[sizeof g_name_buf]) {
+  memcpy(g_name_buf, name, sizeof name);
+  g_last_kernel = g_name_buf;
+}
+
+int prompt_call(const PromptArgs& a, void* stream) {
+  const bool paged = a.block_size > 0;
+  if (a.dtype != MLT_BF16 && a.dtype != MLT_FP16) return MLT_ERR_INVALID_ARG;
+  if (a.T < 0 || a.Tk < 0 || a.B < 0 || a.Hq < 0 || a.H < 0 || a.D <= 0) return MLT_ERR_INVALID_ARG;
+  if (!(a.scale == a.scale) || a.scale - a.scale != 0.f) return MLT_ERR_INVALID_ARG;   // NaN or infinite
+  if (a.D != 64 && a.D != 128) return MLT_ERR_UNSUPPORTED;
+  if (a.T == 0 || a.B == 0 || a.Hq == 0) return MLT_OK;
+  if (a.H == 0 || a.Hq % a.H) return MLT_ERR_INVALID_ARG;
+  constexpr int64_t most = INT_MAX / 4;                  // rows of a head group and of a cache are counted in 32 bits
+  if (a.T > most || a.Tk > most || a.B > most || a.Hq > most / a.D || a.T * (a.Hq / a.H) > most) return MLT_ERR_UNSUPPORTED;
+  if (!a.Q || !a.O || !a.q_offsets || !aligned(a.Q, 16) || !aligned(a.O, 16) || !aligned(a.q_offsets, 4) || a.ldq < a.Hq * a.D || a.ldo < a.Hq * a.D)
+    return MLT_ERR_INVALID_ARG;
+  if (paged) {
+    if (!a.K || !a.V || !a.seq_lens || !a.block_table || !aligned(a.K, 16) || !aligned(a.V, 16) || !aligned(a.seq_lens, 4) || !aligned(a.block_table, 4))
+      return MLT_ERR_INVALID_ARG;
+    if (a.max_blocks > most || a.num_blocks > INT_MAX || a.max_blocks * a.block_size > most) return MLT_ERR_UNSUPPORTED;
+  } else {
+    if (!a.k_offsets || !aligned(a.k_offsets, 4)) return MLT_ERR_INVALID_ARG;
+    if (a.Tk > 0 && (!a.K || !a.V || !aligned(a.K, 16) || !aligned(a.V, 16) || a.ldk < a.H * a.D || a.ldv < a.H * a.D)) return MLT_ERR_INVALID_ARG;
+    if (a.Tk > 0 && (a.ldk % 8 || a.ldv % 8 || a.ldk >= 1 << 23 || a.ldv >= 1 << 23)) return MLT_ERR_UNSUPPORTED;   // 32-bit offsets inside a tile of 64 keys
+  }
+  if (a.ldq % 8 || a.ldo % 8) return MLT_ERR_UNSUPPORTED;
+  if (!device_is_gfx950()) return MLT_ERR_DEVICE;
+  hipStream_t s = (hipStream_t)stream;
+  char name[sizeof g_name_buf];
+  int rc;
+  {
+    TimedRegion t(s);
+    rc = run_prompt(a, s, name, sizeof name);
+  }
+  if (rc == MLT_OK) note_name(name);
+  return rc;
+}
+
+int check_prefix_sizes(int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks, int64_t num_blocks, int64_t prefix_len) {
+  if (B < 0 || Hq < 0 || H < 0 || D <= 0 || block_size <= 0 || max_blocks <= 0 || num_blocks <= 0 || prefix_len < 0) return MLT_ERR_INVALID_ARG;
+  if (D != 64 && D != 128) return MLT_ERR_UNSUPPORTED;
+  if (block_size % 16 || block_size > 1024) return MLT_ERR_UNSUPPORTED;
+  if (B == 0 || Hq == 0) return MLT_OK;
+  if (H == 0 || Hq % H) return MLT_ERR_INVALID_ARG;
+  if (B > INT_MAX || Hq > INT_MAX || B * Hq > INT_MAX / 4 || max_blocks > INT_MAX || max_blocks * block_size > INT_MAX - 1024 || num_blocks > INT_MAX) return MLT_ERR_UNSUPPORTED;
+  if (num_blocks * H > INT_MAX || num_blocks * H * (block_size / 16) > INT_MAX) return MLT_ERR_UNSUPPORTED;   // units of 16 rows are counted in 32 bits
+  return prefix_len > max_blocks * block_size ? MLT_ERR_INVALID_ARG : MLT_OK;
+}
+
 int append_call(const AppendArgs& a, bool fp8, void* stream) {
   if (a.dtype != MLT_BF16 && a.dtype != MLT_FP16) return MLT_ERR_INVALID_ARG;
   if (a.T < 0 || a.B < 0 || a.Hq < 0 || a.H < 0 || a.D <= 0 || a.block_size <= 0 || a.max_blocks <= 0 || a.num_blocks <= 0 || a.rot < 0 || a.rot > a.D)
@@ -448,6 +498,87 @@ int mlt_paged_attn_decode_fp8(int64_t B, int64_t Hq, int64_t H, int64_t D, int64
     else snprintf(g_name_buf, sizeof g_name_buf, "paged_decode_fp8_d%d_w%d", (int)D, waves);
     g_last_kernel = g_name_buf;
   }
+  return rc;
+}
+
+int mlt_mha_packed_fwd(int64_t Tq, int64_t Tk, int64_t B, int64_t Hq, int64_t H, int64_t D, const void* Q, int64_t ldq, const void* K, int64_t ldk,
+                       const void* V, int64_t ldv, const int32_t* q_offsets, const int32_t* k_offsets, void* O, int64_t ldo, float scale,
+                       int causal, int dtype, void* stream) {
+  PromptArgs a{Tq, Tk, B, Hq, H, D, (const uint16_t*)Q, ldq, (const uint16_t*)K, ldk, (const uint16_t*)V, ldv, q_offsets, k_offsets, 0, 0, 0,
+               nullptr, nullptr, (uint16_t*)O, ldo, scale, causal ? 1 : 0, dtype};
+  return prompt_call(a, stream);
+}
+
+int mlt_paged_attn_prompt(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks, int64_t num_blocks,
+                          const void* Q, int64_t ldq, const void* Kc, const void* Vc, const int32_t* offsets, const int32_t* seq_lens,
+                          const int32_t* block_table, void* O, int64_t ldo, float scale, int dtype, void* stream) {
+  if (block_size <= 0 || max_blocks <= 0 || num_blocks <= 0) return MLT_ERR_INVALID_ARG;
+  if (block_size % 16 || block_size > 1024) return MLT_ERR_UNSUPPORTED;
+  PromptArgs a{T, 0, B, Hq, H, D, (const uint16_t*)Q, ldq, (const uint16_t*)Kc, 0, (const uint16_t*)Vc, 0, offsets, nullptr, block_size, max_blocks, num_blocks,
+               seq_lens, block_table, (uint16_t*)O, ldo, scale, 1, dtype};
+  return prompt_call(a, stream);
+}
+
+int mlt_paged_attn_decode_prefix(int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks, int64_t num_blocks,
+                                 const void* Q, const void* Kc, const void* Vc, const int32_t* prefix_table, int64_t prefix_len,
+                                 const int32_t* block_table, const int32_t* seq_lens, void* O, float scale, void* work, int64_t work_bytes,
+                                 int dtype, void* stream) {
+  if (dtype != MLT_BF16 && dtype != MLT_FP16) return MLT_ERR_INVALID_ARG;
+  if (!(scale == scale) || scale - scale != 0.f) return MLT_ERR_INVALID_ARG;   // NaN or infinite
+  const int rc0 = check_prefix_sizes(B, Hq, H, D, block_size, max_blocks, num_blocks, prefix_len);
+  if (rc0 != MLT_OK) return rc0;
+  if (B == 0 || Hq == 0) return MLT_OK;
+  if (!Q || !Kc || !Vc || !block_table || !seq_lens || !O || (prefix_len > 0 && !prefix_table) || work_bytes < 0) return MLT_ERR_INVALID_ARG;
+  if (!aligned(Q, 16) || !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(O, 2) || !aligned(block_table, 4) || !aligned(seq_lens, 4) ||
+      !aligned(work, 16) || (prefix_len > 0 && !aligned(prefix_table, 4))) return MLT_ERR_INVALID_ARG;
+  if (!device_is_gfx950()) return MLT_ERR_DEVICE;
+  PrefixArgs a{B, Hq, H, D, block_size, max_blocks, num_blocks, (const uint16_t*)Q, (const uint16_t*)Kc, (const uint16_t*)Vc, prefix_table, prefix_len,
+               block_table, seq_lens, (uint16_t*)O, scale, (float*)work, work_bytes, dtype};
+  hipStream_t s = (hipStream_t)stream;
+  char name[sizeof g_name_buf];
+  int rc;
+  {
+    TimedRegion t(s);
+    rc = run_paged_prefix(a, s, name, sizeof name);
+  }
+  if (rc == MLT_OK) note_name(name);
+  return rc;
+}
+
+int64_t mlt_paged_attn_decode_prefix_work(int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks, int64_t prefix_len) {
+  const int rc = check_prefix_sizes(B, Hq, H, D, block_size, max_blocks, 1, prefix_len);
+  if (rc != MLT_OK) return rc;
+  if (B == 0 || Hq == 0) return 0;
+  if (!device_is_gfx950()) return MLT_ERR_DEVICE;
+  PrefixArgs a{};
+  a.B = B; a.Hq = Hq; a.H = H; a.D = D; a.block_size = block_size; a.max_blocks = max_blocks; a.prefix_len = prefix_len;
+  return paged_prefix_work(a);
+}
+
+int mlt_gemm_w4(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const void* Wq, int64_t ldw, int64_t group, const void* S, int64_t lds,
+                const uint8_t* Z, int64_t ldz, void* C, int64_t ldc, int dtype, void* stream) {
+  if (dtype != MLT_BF16 && dtype != MLT_FP16) return MLT_ERR_INVALID_ARG;
+  if (M < 0 || N < 0 || K < 0 || group <= 0) return MLT_ERR_INVALID_ARG;
+  if (group != 32 && group != 64 && group != 128) return MLT_ERR_UNSUPPORTED;
+  if (M == 0 || N == 0) return MLT_OK;
+  if (M > INT_MAX - 256 || N > INT_MAX - 256 || K > INT_MAX - 512) return MLT_ERR_UNSUPPORTED;
+  if (!C || ldc < N || !aligned(C, 2)) return MLT_ERR_INVALID_ARG;
+  if (K > 0) {
+    if (!A || !Wq || !S || lda < K || ldw < K / 2 || lds < N || (Z && ldz < N)) return MLT_ERR_INVALID_ARG;
+    if (!aligned(A, 16) || !aligned(Wq, 16) || !aligned(S, 2)) return MLT_ERR_INVALID_ARG;
+    if (K % 32 || lda % 8 || ldw % 16) return MLT_ERR_UNSUPPORTED;
+    if (64 * lda * 2 >= (int64_t)1 << 31 || 64 * ldw >= (int64_t)1 << 31) return MLT_ERR_UNSUPPORTED;   // 32-bit offsets inside a tile
+  }
+  if (!device_is_gfx950()) return MLT_ERR_DEVICE;
+  Gemm4bitArgs a{M, N, K, (const uint16_t*)A, lda, (const uint8_t*)Wq, ldw, group, (const uint16_t*)S, lds, Z, ldz, (uint16_t*)C, ldc, dtype};
+  hipStream_t s = (hipStream_t)stream;
+  char name[sizeof g_name_buf];
+  int rc;
+  {
+    TimedRegion t(s);
+    rc = run_gemm_4bit(a, s, name, sizeof name);
+  }
+  if (rc == MLT_OK) note_name(name);
   return rc;
 }
 

@@ -238,6 +238,44 @@ struct PagedFp8Args {
 bool paged_fp8_by_length(const PagedFp8Args& a, int64_t wgs, int64_t nsplit, bool wide, int64_t ncu);   // wgs workgroups (wide: of 512 threads) dealt out by sequence length?
 int run_paged_fp8(const PagedFp8Args& a, hipStream_t s, int* nsplit_out, int* waves_out);   // paged_fp8.hip; key ranges per pair and wavefronts per workgroup that ran
 
+// Attention of packed sequences: keys packed too (K, V, k_offsets), or in a paged cache (K, V the cache, block_size > 0)
+struct PromptArgs {
+  int64_t T, Tk, B, Hq, H, D;
+  const uint16_t* Q; int64_t ldq;
+  const uint16_t* K; int64_t ldk;
+  const uint16_t* V; int64_t ldv;
+  const int32_t *q_offsets, *k_offsets;
+  int64_t block_size, max_blocks, num_blocks;
+  const int32_t *seq_lens, *block_table;
+  uint16_t* O; int64_t ldo;
+  float scale;
+  int causal, dtype;
+};
+int run_prompt(const PromptArgs& a, hipStream_t s, char* name, size_t size);   // prompt.hip; name: of the kernel that ran
+struct PrefixArgs {
+  int64_t B, Hq, H, D, block_size, max_blocks, num_blocks;
+  const uint16_t *Q, *Kc, *Vc;
+  const int32_t* prefix_table; int64_t prefix_len;
+  const int32_t *block_table, *seq_lens;
+  uint16_t* O;
+  float scale;
+  float* work; int64_t work_bytes;
+  int dtype;
+};
+int run_paged_prefix(const PrefixArgs& a, hipStream_t s, char* name, size_t size);   // paged_prefix.hip
+int64_t paged_prefix_work(const PrefixArgs& a);   // bytes of work; by the sizes alone
+struct Gemm4bitArgs {
+  int64_t M, N, K;
+  const uint16_t* A; int64_t lda;
+  const uint8_t* W; int64_t ldw;
+  int64_t group;
+  const uint16_t* S; int64_t lds;
+  const uint8_t* Z; int64_t ldz;
+  uint16_t* C; int64_t ldc;
+  int dtype;
+};
+int run_gemm_4bit(const Gemm4bitArgs& a, hipStream_t s, char* name, size_t size);   // gemm_4bit.hip
+
 // The library's own scratch memory for a stream of the current device: at least `bytes`, behind its counters, kept
 // (and grown by doubling) from call to call, never freed; nullptr if it cannot be had, and while the
 // stream records into a graph. Work of one stream that uses it is ordered by the stream.
