@@ -170,7 +170,7 @@ int prompt_call(const PromptArgs& a, void* stream) {
     if (a.Tk > 0 && (!a.K || !a.V || !aligned(a.K, 16) || !aligned(a.V, 16) || a.ldk < a.H * a.D || a.ldv < a.H * a.D)) return MLT_ERR_INVALID_ARG;
     if (a.Tk > 0 && (a.ldk % 8 || a.ldv % 8 || a.ldk >= 1 << 23 || a.ldv >= 1 << 23)) return MLT_ERR_UNSUPPORTED;   // 32-bit offsets inside a tile of 64 keys
   }
-  if (a.ldq % 8 || a.ldo % 8) return MLT_ERR_UNSUPPORTED;
+  if (a.ldq % 8 || a.ldo % 8 || a.ldo >= 1 << 29) return MLT_ERR_UNSUPPORTED;   // 32-bit offsets inside 32 rows
   if (!device_is_gfx950()) return MLT_ERR_DEVICE;
   hipStream_t s = (hipStream_t)stream;
   char name[sizeof g_name_buf];
