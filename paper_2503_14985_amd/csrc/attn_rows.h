@@ -17,9 +17,9 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 
-// krow(j), vrow(j): first element of key (value) j in K (V)
+// krow(j), vrow(j): key (value) j's row. Ends early where nothing but NaN can come of it.
 template <typename Tag, int D, typename KRow, typename VRow>
-__device__ __forceinline__ void attend_row(const uint16_t* q, uint16_t* out, int64_t end, const uint16_t* K, const uint16_t* V, KRow krow, VRow vrow, float c) {
+__device__ __forceinline__ void attend_row(const uint16_t* q, uint16_t* out, int64_t end, KRow krow, VRow vrow, float c) {
   constexpr int E = D / 64;
   const int lane = threadIdx.x & 63;
   float m = -__builtin_inff(), l = 0.f, o[E] = {};
@@ -27,8 +27,9 @@ __device__ __forceinline__ void attend_row(const uint16_t* q, uint16_t* out, int
     const int64_t j = j0 + lane;
     float s = -__builtin_inff();
     if (j < end) {
-      const uint16_t* k = K + krow(j);
+      const uint16_t* k = krow(j);
       s = 0.f;
+#pragma clang loop unroll(disable)
       for (int d = 0; d < D; ++d) s = __builtin_fmaf(Elem<Tag>::to_f32(q[d]), Elem<Tag>::to_f32(k[d]), s);
       s *= c;
     }
@@ -39,12 +40,17 @@ __device__ __forceinline__ void attend_row(const uint16_t* q, uint16_t* out, int
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] *= alpha;
     const int n = end - j0 < 64 ? (int)(end - j0) : 64;
+#pragma clang loop unroll(disable)
     for (int i = 0; i < n; ++i) {
-      const uint16_t* v = V + vrow(j0 + i);
+      const uint16_t* v = vrow(j0 + i);
       const float w = __shfl(p, i);
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(w, Elem<Tag>::to_f32(v[e * 64 + lane]), o[e]);
     }
+    bool lost = true;
+#pragma unroll
+    for (int e = 0; e < E; ++e) lost = lost && o[e] != o[e];
+    if (__all(lost)) break;
   }
 #pragma unroll
   for (int e = 0; e < E; ++e) out[e * 64 + lane] = Elem<Tag>::from_f32(end > 0 ? o[e] / l : 0.f);

@@ -21,7 +21,7 @@ __global__ __launch_bounds__(256) void prefix_rows_kernel(PrefixArgs a, float c)
     blk = blk < 0 ? 0 : blk >= a.num_blocks ? a.num_blocks - 1 : blk;
     return ((blk * a.H + h) * a.block_size + j % a.block_size) * D;
   };
-  attend_row<Tag, D>(a.Q + w * D, a.O + w * D, len, a.Kc, a.Vc, row, row, c);
+  attend_row<Tag, D>(a.Q + w * D, a.O + w * D, len, [&](int64_t j) { return a.Kc + row(j); }, [&](int64_t j) { return a.Vc + row(j); }, c);
 }
 
 }  // namespace

@@ -8,11 +8,13 @@
 //   * A wavefront's loads of a tile are 8 neighbouring rows of K and of V. In a paged cache they lie in one block (blocks are whole multiples of 16 keys): one block
 //     number for each tile, read by the scalar unit a tile ahead.
 //   * A row may see no key at all: weights are taken against 0 while the maximum is -inf, and a sum of 0 gives an output of 0.
-//   * A masked key's weight is 0, and 0 times a V that is not finite would be NaN. Where an output is not finite, the workgroup does its item once more with
-//     `careful` set (below). Nothing is spent on that before it is needed but one look at the outputs, a barrier and 64 multiplications an item.
+//   * A masked key's weight is 0, and 0 times a V that is not finite would be NaN. A row whose output is not finite, and to whose last tiles such a V belongs that it does not
+//     see, is worked out again by itself (prompt_redo). Nothing is spent on that before it is needed but one look at the outputs, 64 multiplications an item.
 //
 // The largest weight of a row lies between 1 and 2^8 (the reference moves when the maximum has grown by 8): fp16 weights lose nothing but what is below 2^-25 of it.
 #include <stdio.h>
+
+#include <type_traits>
 
 #include "prompt_tile.h"
 
@@ -21,122 +23,82 @@ namespace mlt {
 namespace {
 
 template <typename Tag, int D, bool CAUSAL, bool PAGED>
-__global__ __launch_bounds__(PA_NT, D == 64 ? 4 : 1) void prompt_kernel(const uint16_t* __restrict__ Q, uint16_t* __restrict__ O, PromptKeys src, PromptItems items, int64_t ldq,
-                                                                        int64_t ldo, float c, int negate) {
+__device__ __forceinline__ void prompt_body(const PromptKernel& p, const PromptSeq& seq, int b, int head, int qt, uint32_t lds0) {
   typedef PaCfg<D> L;
   typedef typename Elem<Tag>::vec8 V8;
   constexpr int NKK = L::NKK, NDT = L::NDT, ROWB = L::ROWB;
   constexpr int IN8 = 8 / L::LPW;                        // rows of one load
-  extern __shared__ __align__(16) char smem[];
-
+  const PromptKeys& src = p.src;
+  const PromptItems& items = p.items;
+  const int64_t ldq = p.ldq, ldo = p.ldo;
+  const float c = p.c;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int grp = wave >> 2;                             // waves w and w+4 share a SIMD
   const int lq = lane & 31, h = lane >> 5;
-  PromptSeq seq;
-  int b, head, qt;
-  if (!prompt_item<PA_BM, PA_NT>(items, reinterpret_cast<int*>(smem), seq, b, head, qt)) return;
   const int G = items.G, rows = seq.n * G, m = seq.m;
   const int q0 = qt * PA_BM + wave * 32;                 // first row of this wavefront
   const int my_r = q0 + lq, last_r = rows - 1;
-  const int my_row = my_r < last_r ? my_r : last_r;      // (rows past the last one repeat it and are not stored)
-  const int my_tok = my_row / G, my_g = my_row - my_tok * G;
+  const int my_tok = (my_r < last_r ? my_r : last_r) / G;   // (rows past the last one repeat it and are not stored)
 
   // Keys that row r sees: those before end(r) (all of them without the mask), none where that is 0 or less.
   const int shift = m - seq.n + 1;
-  auto end_of = [&](int r) { return CAUSAL ? shift + (r < last_r ? r : last_r) / G : m; };
-  const int wg_end = end_of((qt + 1) * PA_BM - 1), w_first = end_of(q0), w0 = end_of(qt * PA_BM), w0_first = w0 > 0 ? w0 : 0, w_end = end_of(q0 + 31), my_end = CAUSAL ? shift + my_tok : m;
+  auto end_of = [&](int r) { return CAUSAL ? shift + uniform((r < last_r ? r : last_r) / G) : m; };
+  const int wg_end = end_of((qt + 1) * PA_BM - 1), w_first = end_of(q0), w_end = end_of(q0 + 31), my_end = CAUSAL ? shift + my_tok : m;
+  const int my_last = my_end - 1 - 4 * h;                // ... from the first key that this lane holds of 8
   const int nblk = wg_end > 0 ? (wg_end + PA_BN - 1) / PA_BN : 0;
   // This wavefront has visible keys in tiles 0 .. my_nblk-1 only.
   const int my_nblk = w_end > 0 && q0 < rows ? (w_end + PA_BN - 1) / PA_BN : 0;
 
-  // ---- Q^T operand, resident in registers: row lq, d = 16*kk + 8*h .. +7; a negative scale as a sign flip
-  V8 qf[NKK];
-  {
-    const uint16_t* qp = Q + (int64_t)(seq.q0 + my_tok) * ldq + (int64_t)(head * G + my_g) * D + 8 * h;
-    const uint32_t flip = negate ? 0x80008000u : 0u;
-#pragma unroll
-    for (int kk = 0; kk < NKK; ++kk) {
-      u32x4 raw = *reinterpret_cast<const u32x4_mem*>(qp + kk * 16);
-      raw[0] ^= flip; raw[1] ^= flip; raw[2] ^= flip; raw[3] ^= flip;
-      qf[kk] = __builtin_bit_cast(V8, raw);
-    }
-  }
-  // where this row goes, in 16-byte pieces from the wavefront's first token on (a store below writes whole rows and asks the lane that knows)
-  const int tok0 = (q0 < last_r ? q0 : last_r) / G;
-  const int o_piece = (int)(((my_tok - tok0) * ldo + (int64_t)my_g * D) / 8);
+  V8 qf[NKK];                                            // Q^T operand: row lq, d = 16*kk + 8*h .. +7
 
   // ---- global -> LDS assignments: wavefront w fills rows 8 w .. 8 w + 7 of the K tile and of the V tile; lane l owns the 16-byte slot l of a 1 KB block.
   const uint32_t rowk = PAGED ? ROWB : (uint32_t)src.ldk * 2, rowv = PAGED ? ROWB : (uint32_t)src.ldv * 2;
-  uint32_t chunk_k[L::LPW], chunk_v[L::LPW];
+  uint32_t voff_k[L::LPW], voff_v[L::LPW];               // byte offsets from the first of the 8 rows, all of them there
+  // `have`: rows behind the first one that are there; those past them re-read the last one (their weights are 0)
+  auto offsets_of = [&](int ln, int i, int have, uint32_t& ok, uint32_t& ov) __attribute__((always_inline)) {
+    const int in8 = i * IN8 + ln / L::CPR, slot = ln % L::CPR, at = in8 < have ? in8 : have;
+    ok = (uint32_t)at * rowk + (uint32_t)(slot ^ L::fk(wave * 8 + in8)) * 16u;
+    ov = (uint32_t)at * rowv + (uint32_t)(slot ^ L::fv(wave * 8 + in8)) * 16u;
+  };
 #pragma unroll
-  for (int i = 0; i < L::LPW; ++i) {
-    const int row = wave * 8 + i * IN8 + lane / L::CPR, slot = lane % L::CPR;
-    chunk_k[i] = (uint32_t)(slot ^ L::fk(row)) * 16u;
-    chunk_v[i] = (uint32_t)(slot ^ L::fv(row)) * 16u;
-  }
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr_t)smem;
-  // The place of the first of the wavefront's 8 keys of the tile that is fetched next. Paged: its block's number (read a tile ahead) and slot.
+  for (int i = 0; i < L::LPW; ++i) offsets_of(lane, i, 7, voff_k[i], voff_v[i]);
   const int last_key = wg_end - 1;                       // of what this workgroup reads
-  const int32_t* table = PAGED ? src.block_table + (int64_t)b * src.max_blocks : nullptr;
-  const int bs = PAGED ? src.block_size : 1, blk64 = PA_BN / bs, slot64 = PA_BN - blk64 * bs;
-  int at_key, at_blk = 0, at_slot = 0, at_pb = 0;
-  auto look_up = [&]() __attribute__((always_inline)) {  // (past the last key: the block of that one, and its slot)
-    if (PAGED && last_key >= 0) at_pb = table[at_key <= last_key ? at_blk : last_key / bs];
-  };
-  auto first_tile = [&]() __attribute__((always_inline)) {
-    at_key = wave * 8;
-    if (PAGED) { at_blk = at_key / bs; at_slot = at_key - at_blk * bs; }
-    look_up();
-  };
+  PromptCursor<D, 8, PAGED> at;                          // (K and V of a packed sequence may have other strides: ...)
+  auto first_tile = [&]() __attribute__((always_inline)) { at.start(src, src.K, src.ldk, seq, b, items.H, head, last_key, wave * 8, PA_BN); };
   auto issue_tile = [&](int t) __attribute__((always_inline)) {
     const uint32_t dst = lds0 + (t % PA_NS) * L::SLOT_B + wave * L::LPW * 1024;
-    // rows past the last key re-read its row (their weights are 0)
-    const int over = at_key - last_key;                  // > 0: all of them
-    const char *kp, *vp;
-    if (PAGED) {
-      const int pb = at_pb < 0 ? 0 : at_pb >= src.num_blocks ? src.num_blocks - 1 : at_pb;
-      const int slot = over > 0 ? last_key % bs : at_slot;
-      const int64_t row = ((int64_t)pb * items.H + head) * bs + slot;
-      kp = reinterpret_cast<const char*>(src.K) + row * ROWB;
-      vp = reinterpret_cast<const char*>(src.V) + row * ROWB;
+    int have;
+    const int key = at.key < last_key ? at.key : last_key;
+    const char* kp = at.next(have);
+    const char* vp = uniform(PAGED ? reinterpret_cast<const char*>(src.V) + (kp - reinterpret_cast<const char*>(src.K))
+                                   : reinterpret_cast<const char*>(src.V + (int64_t)(seq.k0 + key) * src.ldv + (int64_t)head * D));   // (... this is V's)
+    if (D == 128 && have == 7) {                         // (D = 64 has no registers to keep them in)
+#pragma unroll
+      for (int i = 0; i < L::LPW; ++i) load_lds16(kp, voff_k[i], dst + i * 1024);
+#pragma unroll
+      for (int i = 0; i < L::LPW; ++i) load_lds16(vp, voff_v[i], dst + L::TILE_B + i * 1024);
     } else {
-      const int64_t row = seq.k0 + (over > 0 ? last_key : at_key);
-      kp = reinterpret_cast<const char*>(src.K + row * src.ldk + (int64_t)head * D);
-      vp = reinterpret_cast<const char*>(src.V + row * src.ldv + (int64_t)head * D);
-    }
-    const int have = over > 0 ? 0 : -over < 7 ? -over : 7;                 // rows behind the first that exist
+      int ln = lane;
+      asm volatile("" : "+v"(ln));
 #pragma unroll
-    for (int i = 0; i < L::LPW; ++i) {
-      const int in8 = i * IN8 + lane / L::CPR;
-      load_lds16(kp, (uint32_t)(in8 < have ? in8 : have) * rowk + chunk_k[i], dst + i * 1024);
+      for (int i = 0; i < L::LPW; ++i) {
+        uint32_t ok, ov;
+        offsets_of(ln, i, have, ok, ov);
+        load_lds16(kp, ok, dst + i * 1024);
+        load_lds16(vp, ov, dst + L::TILE_B + i * 1024);
+      }
     }
-#pragma unroll
-    for (int i = 0; i < L::LPW; ++i) {
-      const int in8 = i * IN8 + lane / L::CPR;
-      load_lds16(vp, (uint32_t)(in8 < have ? in8 : have) * rowv + chunk_v[i], dst + L::TILE_B + i * 1024);
-    }
-    at_key += PA_BN;
-    if (PAGED) {
-      at_blk += blk64;
-      at_slot += slot64;
-      if (at_slot >= bs) { at_slot -= bs; ++at_blk; }
-    }
-    look_up();
   };
-
-  // ---- fragment addresses inside a slot (see mha_pp_kernel)
-  const int k_frag = lq * ROWB + ((h ^ L::fk(lq)) << 4);
-  const int vg = lane >> 4, vs = lane & 15;
-  const int v_row = 4 * (vg >> 1) + (vs >> 2);
-  const int v_frag = L::TILE_B + v_row * ROWB + (((2 * (vg & 1) + ((vs & 3) >> 1)) ^ L::fv(v_row)) << 4) + 8 * (vs & 1);
 
   f32x16 o_acc[NDT];
   f32x16 s_acc[2];
   u32x4 pq[4];                       // P^T of the current tile as MFMA operands: one per 16 keys
   float mc_run, l_run;
   V8 fb[2][NDT];
-  uint32_t ka[NKK], va[NDT];
+  // Fragment addresses: one per XOR variant in a register, moved from slot to slot; D = 64, which has no registers to spare, keeps one of K's and works out the others
+  constexpr int NKA = D == 64 ? 1 : NKK;
+  uint32_t ka[NKA], va[NDT];
   auto read_v_frag = [&](int g, int t, V8& f) {
     const uint32_t a = va[t] + g * 16 * ROWB;
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((MLT_LDS s16x4*)(uintptr_t)a);
@@ -144,7 +106,7 @@ __global__ __launch_bounds__(PA_NT, D == 64 ? 4 : 1) void prompt_kernel(const ui
     f = join_tr<V8>(lo, hi);
   };
   auto read_k_frag = [&](int fi, V8& f) {
-    const uint32_t a = ka[fi >> 1] + (fi & 1) * 32 * ROWB;
+    const uint32_t a = (NKA == 1 ? ka[0] ^ ((fi >> 1) << 5) : ka[(fi >> 1) % NKA]) + (fi & 1) * 32 * ROWB;
     f = __builtin_bit_cast(V8, *(const MLT_LDS u32x4*)(uintptr_t)a);
   };
   auto mfma_v = [&](int g, int t, const V8& f) { o_acc[t] = mfma32(f, __builtin_bit_cast(V8, pq[g]), o_acc[t]); };
@@ -165,7 +127,7 @@ __global__ __launch_bounds__(PA_NT, D == 64 ? 4 : 1) void prompt_kernel(const ui
   auto softmax_tile = [&](int j) {
     // register r of sub-tile kb is key 64 j + 32 kb + 8 (r / 4) + 4 h + r % 4
     if (cut(j)) {
-      const int rel = my_end - 1 - (j * PA_BN + 4 * h);
+      const int rel = my_last - j * PA_BN;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -201,80 +163,114 @@ __global__ __launch_bounds__(PA_NT, D == 64 ? 4 : 1) void prompt_kernel(const ui
         pq[2 * kb + r / 8][(r / 2) & 3] = Elem<Tag>::pack2(p0, p1);
       }
   };
-  // ---- `careful`: in tiles that the mask cuts for any row of the workgroup, what is not finite in V counts as 0 in the product (every wavefront puts its own
-  // rows right when they have landed) and is added afterwards, as it is, to the rows that see its key (a positive weight times it).
-  const int first_cut = w0_first / PA_BN;                // (of the workgroup's first row: 0 where that sees nothing)
-  auto wild = [](uint32_t pair, int half) {              // exponent all ones?
-    constexpr uint32_t E = __is_same(Tag, bf16_tag) ? 0x7f80u : 0x7c00u;
-    return ((pair >> (16 * half)) & E) == E;
-  };
-  auto clean = [&](int t) __attribute__((always_inline)) {
-    if (t < first_cut) return;
-    const uint32_t at = lds0 + (t % PA_NS) * L::SLOT_B + L::TILE_B + wave * L::LPW * 1024 + lane * 16;
-#pragma unroll
-    for (int i = 0; i < L::LPW; ++i) {
-      u32x4 w = *(const MLT_LDS u32x4_mem*)(uintptr_t)(at + i * 1024);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = (wild(w[e], 0) ? 0u : w[e] & 0xffffu) | (wild(w[e], 1) ? 0u : w[e] & 0xffff0000u);
-      *(MLT_LDS u32x4_mem*)(uintptr_t)(at + i * 1024) = w;
-    }
-    __builtin_amdgcn_s_waitcnt(wait_imm(63, 0));
-  };
-  auto add_wild = [&]() {
-#pragma clang loop unroll(disable)
-    for (int key = first_cut * PA_BN; key < wg_end; ++key) {
-      const uint16_t* v;
-      if (PAGED) {
-        int pb = table[key / bs];
-        pb = pb < 0 ? 0 : pb >= src.num_blocks ? src.num_blocks - 1 : pb;
-        v = src.V + (((int64_t)pb * items.H + head) * bs + key % bs) * D;
-      } else {
-        v = src.V + (int64_t)(seq.k0 + key) * src.ldv + (int64_t)head * D;
-      }
-      if (key >= my_end) continue;
-#pragma unroll
-      for (int t = 0; t < NDT; ++t)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const u32x2 w = *reinterpret_cast<const u32x2_mem*>(v + 32 * t + 8 * g + 4 * h);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (wild(w[e >> 1], e & 1)) o_acc[t][4 * g + e] += Elem<Tag>::to_f32((uint16_t)(w[e >> 1] >> (16 * (e & 1))));
-        }
-    }
-  };
-
   constexpr int LPT = 2 * L::LPW;                         // loads per wavefront per tile
-  for (int careful = 0;; careful = 1) {
 #pragma unroll
-    for (int t = 0; t < NDT; ++t)
+  for (int t = 0; t < NDT; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o_acc[t][r] = 0.f;
-    mc_run = -__builtin_inff();    // reference point of the weights: a running maximum of the scores, times c (log2 domain)
-    l_run = 0.f;                   // running sum over this lane's half of the keys
+    for (int r = 0; r < 16; ++r) o_acc[t][r] = 0.f;
+  mc_run = -__builtin_inff();    // reference point of the weights: a running maximum of the scores, times c (log2 domain)
+  l_run = 0.f;                   // running sum over this lane's half of the keys
+  {
+    // Q, and fragment addresses inside a slot (see mha_pp_kernel), from an opaque lane number: not to be kept in registers for a second turn
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const int fq = ln & 31, fh = ln >> 5;
+    const int row = q0 + fq < last_r ? q0 + fq : last_r, tok = row / G;
+    const uint16_t* qp = p.Q + (int64_t)(seq.q0 + tok) * ldq + (int64_t)(head * G + row - tok * G) * D + 8 * fh;
+    const uint32_t flip = p.negate ? 0x80008000u : 0u;       // a negative scale as a sign flip
 #pragma unroll
-    for (int kk = 0; kk < NKK; ++kk) ka[kk] = lds0 + (uint32_t)(k_frag ^ (kk << 5));
+    for (int kk = 0; kk < NKK; ++kk) {
+      u32x4 raw = *reinterpret_cast<const u32x4_mem*>(qp + kk * 16);
+      raw[0] ^= flip; raw[1] ^= flip; raw[2] ^= flip; raw[3] ^= flip;
+      qf[kk] = __builtin_bit_cast(V8, raw);
+    }
+    const int k_frag = fq * ROWB + ((fh ^ L::fk(fq)) << 4);
+    const int vg = ln >> 4, vs = ln & 15;
+    const int v_row = 4 * (vg >> 1) + (vs >> 2);
+    const int v_frag = L::TILE_B + v_row * ROWB + (((2 * (vg & 1) + ((vs & 3) >> 1)) ^ L::fv(v_row)) << 4) + 8 * (vs & 1);
+#pragma unroll
+    for (int kk = 0; kk < NKA; ++kk) ka[kk] = lds0 + (uint32_t)(k_frag ^ (kk << 5));
 #pragma unroll
     for (int t = 0; t < NDT; ++t) va[t] = lds0 + (uint32_t)(v_frag ^ (t << 6));
+  }
 
-    // ---- schedule: see mha_pp_kernel
-    first_tile();
+  // ---- schedule: see mha_pp_kernel
+  first_tile();
 #pragma unroll
-    for (int t = 0; t < PA_AHEAD; ++t)
-      if (t < nblk) issue_tile(t);
-    if (nblk >= 3) __builtin_amdgcn_s_waitcnt(wait_imm(2 * LPT, 15));
-    else if (nblk == 2) __builtin_amdgcn_s_waitcnt(wait_imm(LPT, 15));
-    else __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));
-    if (CAUSAL && careful && nblk > 0) clean(0);
+  for (int t = 0; t < PA_AHEAD; ++t)
+    if (t < nblk) issue_tile(t);
+  if (nblk >= 3) __builtin_amdgcn_s_waitcnt(wait_imm(2 * LPT, 15));
+  else if (nblk == 2) __builtin_amdgcn_s_waitcnt(wait_imm(LPT, 15));
+  else __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));
+  MLT_BARRIER();
+  if (grp == 1) MLT_BARRIER();            // stagger: group 1 runs one phase behind
+  {
+    if (my_nblk > 0) {                                    // ka, va point into slot 0
+#pragma unroll
+      for (int i = 0; i < NDT; ++i) read_k_frag(i, fb[0][i]);
+#pragma unroll
+      for (int i = 0; i < NDT; ++i) read_k_frag(NDT + i, fb[1][i]);
+      MLT_SB();
+#pragma unroll
+      for (int ch = 0; ch < 4; ++ch)
+#pragma unroll
+        for (int i = 0; i < NDT; ++i) {
+          mfma_k(ch * NDT + i, fb[ch & 1][i]);
+          MLT_SB();
+          if (ch < 2) read_k_frag((ch + 2) * NDT + i, fb[ch & 1][i]);
+          else read_v_frag(ch - 2, i, fb[ch & 1][i]);
+          MLT_SB();
+        }
+    }
+    if (grp == 1) {
+      if (nblk >= 3) __builtin_amdgcn_s_waitcnt(wait_imm(LPT, 15));
+      else __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));
+    }
     MLT_BARRIER();
-    if (grp == 1) MLT_BARRIER();            // stagger: group 1 runs one phase behind
-    {
-      if (my_nblk > 0) {                                    // ka, va point into slot 0
+  }
+
+  int slot_off = 0;                                       // byte offset of tile j's slot
+  for (int j = 0; j < nblk; ++j) {
+    const int slot_off_next = slot_off + L::SLOT_B == L::SMEM ? 0 : slot_off + L::SLOT_B;
+    const bool active = j < my_nblk;                       // wavefront-uniform
+    const bool active_next = j + 1 < my_nblk;
+    // ---- X_j (the first two V_j groups are already in the chunk buffers)
+    if (j + PA_AHEAD < nblk) issue_tile(j + PA_AHEAD);
+    __builtin_amdgcn_sched_barrier(0);
+    if (active) {
+      softmax_tile(j);
 #pragma unroll
-        for (int i = 0; i < NDT; ++i) read_k_frag(i, fb[0][i]);
+      for (int g = 0; g < 4; ++g) asm volatile("" : "+v"(pq[g]));
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (grp == 0) {
+      const int newer = (j + 3 < nblk ? 1 : 0) + (j + 2 < nblk ? 1 : 0);
+      if (newer == 2) __builtin_amdgcn_s_waitcnt(wait_imm(2 * LPT, 0));
+      else if (newer == 1) __builtin_amdgcn_s_waitcnt(wait_imm(LPT, 0));
+      else __builtin_amdgcn_s_waitcnt(wait_imm(0, 0));
+    } else {
+      __builtin_amdgcn_s_waitcnt(wait_imm(63, 0));
+    }
+    MLT_BARRIER();
+    __builtin_amdgcn_sched_barrier(0);
+    if (D == 128) __builtin_amdgcn_s_setprio(1);
+    // ---- C_j
+    if (active) {
+      const uint32_t dslot = (uint32_t)(slot_off_next - slot_off);
 #pragma unroll
-        for (int i = 0; i < NDT; ++i) read_k_frag(NDT + i, fb[1][i]);
-        MLT_SB();
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int t = 0; t < NDT; ++t) {
+          mfma_v(g, t, fb[g & 1][t]);
+          MLT_SB();
+          if (g < 2) read_v_frag(g + 2, t, fb[g & 1][t]);
+          else read_k_frag((g - 2) * NDT + t, fb[g & 1][t]);
+          if (g == 0 && NKA > 1) { ka[(2 * t) % NKA] += dslot; ka[(2 * t + 1) % NKA] += dslot; }
+          if (g == 0 && NKA == 1 && t == 0) ka[0] += dslot;
+          if (g == 3) va[t] += dslot;
+          MLT_SB();
+        }
+      if (active_next) {
 #pragma unroll
         for (int ch = 0; ch < 4; ++ch)
 #pragma unroll
@@ -286,107 +282,35 @@ __global__ __launch_bounds__(PA_NT, D == 64 ? 4 : 1) void prompt_kernel(const ui
             MLT_SB();
           }
       }
-      if (grp == 1) {
-        if (nblk >= 3) __builtin_amdgcn_s_waitcnt(wait_imm(LPT, 15));
-        else __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));
-        if (CAUSAL && careful && nblk > 1) clean(1);
-      }
-      MLT_BARRIER();
+      // the sum of the ROUNDED weights (what P V used), while the matrix pipe drains
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) l_run = Elem<Tag>::add_pair(pq[g][e], l_run);
+      asm volatile("" : "+v"(l_run));
     }
-
-    int slot_off = 0;                                       // byte offset of tile j's slot
-    for (int j = 0; j < nblk; ++j) {
-      const int slot_off_next = slot_off + L::SLOT_B == L::SMEM ? 0 : slot_off + L::SLOT_B;
-      const bool active = j < my_nblk;                       // wavefront-uniform
-      const bool active_next = j + 1 < my_nblk;
-      // ---- X_j (the first two V_j groups are already in the chunk buffers)
-      if (j + PA_AHEAD < nblk) issue_tile(j + PA_AHEAD);
-      __builtin_amdgcn_sched_barrier(0);
-      if (active) {
-        softmax_tile(j);
-#pragma unroll
-        for (int g = 0; g < 4; ++g) asm volatile("" : "+v"(pq[g]));
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      if (grp == 0) {
-        const int newer = (j + 3 < nblk ? 1 : 0) + (j + 2 < nblk ? 1 : 0);
-        if (newer == 2) __builtin_amdgcn_s_waitcnt(wait_imm(2 * LPT, 0));
-        else if (newer == 1) __builtin_amdgcn_s_waitcnt(wait_imm(LPT, 0));
-        else __builtin_amdgcn_s_waitcnt(wait_imm(0, 0));
-        if (CAUSAL && careful && j + 1 < nblk) clean(j + 1);
-      } else {
-        __builtin_amdgcn_s_waitcnt(wait_imm(63, 0));
-      }
-      MLT_BARRIER();
-      __builtin_amdgcn_sched_barrier(0);
-      if (D == 128) __builtin_amdgcn_s_setprio(1);
-      // ---- C_j
-      if (active) {
-        const uint32_t dslot = (uint32_t)(slot_off_next - slot_off);
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-#pragma unroll
-          for (int t = 0; t < NDT; ++t) {
-            mfma_v(g, t, fb[g & 1][t]);
-            MLT_SB();
-            if (g < 2) read_v_frag(g + 2, t, fb[g & 1][t]);
-            else read_k_frag((g - 2) * NDT + t, fb[g & 1][t]);
-            if (g == 0) { ka[2 * t] += dslot; ka[2 * t + 1] += dslot; }
-            if (g == 3) va[t] += dslot;
-            MLT_SB();
-          }
-        if (active_next) {
-#pragma unroll
-          for (int ch = 0; ch < 4; ++ch)
-#pragma unroll
-            for (int i = 0; i < NDT; ++i) {
-              mfma_k(ch * NDT + i, fb[ch & 1][i]);
-              MLT_SB();
-              if (ch < 2) read_k_frag((ch + 2) * NDT + i, fb[ch & 1][i]);
-              else read_v_frag(ch - 2, i, fb[ch & 1][i]);
-              MLT_SB();
-            }
-        }
-        // the sum of the ROUNDED weights (what P V used), while the matrix pipe drains
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) l_run = Elem<Tag>::add_pair(pq[g][e], l_run);
-        asm volatile("" : "+v"(l_run));
-      }
-      if (D == 128) __builtin_amdgcn_s_setprio(0);
-      __builtin_amdgcn_sched_barrier(0);
-      if (grp == 1) {
-        if (j + 3 < nblk) __builtin_amdgcn_s_waitcnt(wait_imm(LPT, 15));
-        else __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));
-        if (CAUSAL && careful && j + 2 < nblk) clean(j + 2);
-      }
-      MLT_BARRIER();
-      __builtin_amdgcn_sched_barrier(0);
-      slot_off = slot_off_next;
+    if (D == 128) __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+    if (grp == 1) {
+      if (j + 3 < nblk) __builtin_amdgcn_s_waitcnt(wait_imm(LPT, 15));
+      else __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));
     }
-    if (grp == 0) MLT_BARRIER();            // same barrier count for both groups
-
-    // ---- is any output not finite, for which a masked V might be the reason? (The ring is free from here on.)
-    if (!CAUSAL) break;
-    if (careful) {
-      add_wild();
-      break;
-    }
-    float sum = 0.f;                        // x * 0 is 0, or NaN where x is not finite
-#pragma unroll
-    for (int t = 0; t < NDT; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sum = __builtin_fmaf(o_acc[t][r], 0.f, sum);
-    const bool bad = __builtin_amdgcn_ballot_w64(!(sum == 0.f)) != 0;
-    if (lane == 0) *reinterpret_cast<int*>(smem + wave * 4) = bad ? 1 : 0;
-    __syncthreads();
-    int again = 0;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) again |= *reinterpret_cast<const int*>(smem + w * 4);
-    __syncthreads();
-    if (!again) break;
+    MLT_BARRIER();
+    __builtin_amdgcn_sched_barrier(0);
+    slot_off = slot_off_next;
   }
+  if (grp == 0) MLT_BARRIER();            // same barrier count for both groups
+
+
+  // ---- rows to be done again: an output is not finite, and so is a value that the row's last tiles hold without its seeing it
+  float sum = 0.f;                          // x * 0 is 0, or NaN where x is not finite
+#pragma unroll
+  for (int t = 0; t < NDT; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum = __builtin_fmaf(o_acc[t][r], 0.f, sum);
+  const uint64_t bad = __builtin_amdgcn_ballot_w64(!(sum == 0.f));
+  uint32_t redo = 0;
+  if (bad) redo = prompt_redo<Tag, D, CAUSAL, PAGED>(p, seq, b, head, q0, (uint32_t)bad | (uint32_t)(bad >> 32), my_nblk * PA_BN, wg_end);
 #undef MLT_SB
 
   // ---- epilogue: O = O^T / l, l summed over both key halves, rows without keys 0; whole rows through LDS, 16 bytes a lane
@@ -406,14 +330,32 @@ __global__ __launch_bounds__(PA_NT, D == 64 ? 4 : 1) void prompt_kernel(const ui
       const int ch = 4 * t + 2 * gp + h;
       *(MLT_LDS u32x4*)(uintptr_t)(o_lds + lq * ROWB + ((ch ^ (lq & CM)) << 4)) = ow[t][gp];
     }
-  uint16_t* ob = O + (int64_t)(seq.q0 + tok0) * ldo + (int64_t)head * G * D;
+  // where row lq goes, in 16-byte pieces from the wavefront's first token on (a store writes whole rows and asks the lane that knows). Worked out again rather than kept in
+  // registers through the loop.
+  int ln = lane;
+  asm volatile("" : "+v"(ln));
+  const int out_row = q0 + (ln & 31) < last_r ? q0 + (ln & 31) : last_r, out_tok = out_row / G, tok0 = uniform((q0 < last_r ? q0 : last_r) / G);
+  const int o_piece = (int)(((out_tok - tok0) * ldo + (int64_t)(out_row - out_tok * G) * D) / 8);
+  uint16_t* ob = p.O + (int64_t)(seq.q0 + tok0) * ldo + (int64_t)head * G * D;
 #pragma unroll
   for (int i = 0; i < 32 / L::RPB; ++i) {
     const int r = i * L::RPB + lane / L::CPR, cc = lane % L::CPR;
     const u32x4 v = *(const MLT_LDS u32x4*)(uintptr_t)(o_lds + r * ROWB + ((cc ^ (r & CM)) << 4));
     const int piece = __shfl(o_piece, r);
-    if (q0 + r < rows) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_mem*>(ob + ((int64_t)piece + cc) * 8));
+    if (q0 + r < rows && !(redo >> r & 1)) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_mem*>(ob + ((int64_t)piece + cc) * 8));
   }
+}
+
+template <typename Tag, int D, bool CAUSAL, bool PAGED>
+__global__ __launch_bounds__(PA_NT, D == 64 ? 4 : 1) void prompt_kernel(PromptKernel p) {
+  extern __shared__ __align__(16) char smem[];
+  PromptSeq seq;
+  int b, head, qt;
+  if (!prompt_item<PA_BM, PA_NT>(p.items, reinterpret_cast<int*>(smem), seq, b, head, qt)) return;
+  seq.q0 = uniform(seq.q0); seq.n = uniform(seq.n); seq.k0 = uniform(seq.k0); seq.m = uniform(seq.m);
+  b = uniform(b); head = uniform(head); qt = uniform(qt);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr_t)smem;
+  prompt_body<Tag, D, CAUSAL, PAGED>(p, seq, b, head, qt, lds0);
 }
 
 template <typename Tag, int D, bool CAUSAL, bool PAGED>
@@ -437,7 +379,7 @@ int launch_prompt(const PromptArgs& a, hipStream_t s) {
   float c = (a.scale < 0 ? -a.scale : a.scale) * 1.4426950408889634f;   // c > 0 always, as in launch_mha_pp
   if (c < 1e-30f) c = 1e-30f;
   PromptKeys src{a.K, a.V, a.ldk, a.ldv, a.block_table, (int)a.block_size, (int)a.max_blocks, (int)a.num_blocks};
-  hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(PA_NT), L::SMEM, s, a.Q, a.O, src, items, a.ldq, a.ldo, c, a.scale < 0 ? 1 : 0);
+  hipLaunchKernelGGL(kern, dim3((unsigned)grid), dim3(PA_NT), L::SMEM, s, PromptKernel{a.Q, a.O, src, items, a.ldq, a.ldo, c, a.scale < 0 ? 1 : 0});
   return hipGetLastError() == hipSuccess ? MLT_OK : MLT_ERR_LAUNCH;
 }
 

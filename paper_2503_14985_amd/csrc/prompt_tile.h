@@ -5,9 +5,12 @@
 // means that little of the diagonal is computed for nothing.
 #pragma once
 
+#include "attn_rows.h"
 #include "mha_tile.h"
 
 namespace mlt {
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }   // of a value that is one for the wavefront: in a scalar register
 
 struct PromptItems {
   int T, Tk, B, H, G;
@@ -166,7 +169,6 @@ __device__ __forceinline__ bool prompt_item(const PromptItems& a, int* buf, Prom
   }
   b = __builtin_amdgcn_readfirstlane(b);
   if (found && a.B <= NT) {
-    auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
     seq.q0 = uniform(qq[b]);
     seq.n = uniform(nn[b]);
     seq.k0 = uniform(kk[b]);
@@ -179,12 +181,148 @@ __device__ __forceinline__ bool prompt_item(const PromptItems& a, int* buf, Prom
   return found && tile >= 0;
 }
 
-// Where a sequence's keys (or values) lie: packed rows, or blocks of a cache.
+// Where a sequence's keys and values lie: packed rows, or blocks of a cache.
 struct PromptKeys {
   const uint16_t *K, *V;
   int64_t ldk, ldv;                                  // packed
   const int32_t* block_table;                        // paged
   int block_size, max_blocks, num_blocks;
 };
+
+// An address that is one for the wavefront, in scalar registers (the direct loads take no other)
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const char*>((uint64_t)(uint32_t)uniform((int)(uint32_t)a) | (uint64_t)(uint32_t)uniform((int)(uint32_t)(a >> 32)) << 32);
+}
+
+// The way of one wavefront's loads through a sequence's keys (or values): N neighbouring ones that lie in one block of a cache (N divides 16), then those
+// `step` further on. The block's number is read by the scalar unit when the ones before it are fetched. Keys past `last` (-1: there is none) are that one again.
+template <int D, int N, bool PAGED>
+struct PromptCursor {
+  const char* base;
+  int64_t row_bytes;                                 // packed: from a key to the next one; paged: D * 2
+  const int32_t* table;
+  int bs, last, last_blk, last_row, max_pb, per_block, step, step_blk, step_row;
+  int key, blk, row, pb;                             // row: slot in the block
+  __device__ __forceinline__ void start(const PromptKeys& src, const uint16_t* mat, int64_t ld, const PromptSeq& seq, int b, int heads, int h, int last_, int first, int step_) {
+    last = last_;
+    step = step_;
+    key = first;
+    blk = row = pb = 0;
+    if constexpr (PAGED) {
+      base = reinterpret_cast<const char*>(mat);
+      row_bytes = D * 2;
+      table = src.block_table + (int64_t)b * src.max_blocks;
+      bs = src.block_size;
+      max_pb = src.num_blocks - 1;
+      per_block = heads * bs;
+      step_blk = uniform(step / bs);
+      step_row = step - step_blk * bs;
+      blk = uniform(key / bs);
+      last_blk = last >= 0 ? uniform(last / bs) : 0;
+      last_row = last - last_blk * bs;
+      row = key - blk * bs;
+      base += (int64_t)h * bs * (D * 2);
+      look_up();
+    } else {
+      base = reinterpret_cast<const char*>(mat + seq.k0 * ld + (int64_t)h * D);
+      row_bytes = ld * 2;
+    }
+  }
+  __device__ __forceinline__ void look_up() {
+    // (through the constant address space: by the scalar unit. A vector load's wait would be one for the direct loads in flight too.)
+    if (PAGED && last >= 0) pb = ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)table)[key <= last ? blk : last_blk];
+  }
+  // the first of the N keys; `have`: how many of the others exist
+  __device__ __forceinline__ const char* next(int& have) {
+    const int over = key - last;                     // > 0: none of them exists
+    have = over > 0 ? 0 : -over < N - 1 ? -over : N - 1;
+    const char* p;
+    if constexpr (PAGED) {
+      const int blk_ok = pb < 0 ? 0 : pb > max_pb ? max_pb : pb;
+      p = base + ((int64_t)blk_ok * per_block + (over > 0 ? last_row : row)) * (D * 2);
+      blk += step_blk;
+      row += step_row;
+      if (row >= bs) { row -= bs; ++blk; }
+    } else {
+      p = base + (int64_t)(over > 0 ? last : key) * row_bytes;
+    }
+    key += step;
+    look_up();
+    return uniform(p);
+  }
+};
+
+// Key (value) number `key` of a sequence (any below its count)
+template <int D, bool PAGED>
+__device__ __forceinline__ const uint16_t* prompt_row(const PromptKeys& src, const uint16_t* mat, int64_t ld, const PromptSeq& seq, int b, int H, int head, int key) {
+  if constexpr (PAGED) {
+    int pb = src.block_table[(int64_t)b * src.max_blocks + key / src.block_size];
+    pb = pb < 0 ? 0 : pb >= src.num_blocks ? src.num_blocks - 1 : pb;
+    return mat + (((int64_t)pb * H + head) * src.block_size + key % src.block_size) * D;
+  } else {
+    return mat + (int64_t)(seq.k0 + key) * ld + (int64_t)head * D;
+  }
+}
+template <int D, bool PAGED>
+__device__ __forceinline__ const uint16_t* prompt_key(const PromptKeys& src, const PromptSeq& seq, int b, int H, int head, int key) {
+  return prompt_row<D, PAGED>(src, src.K, src.ldk, seq, b, H, head, key);
+}
+template <int D, bool PAGED>
+__device__ __forceinline__ const uint16_t* prompt_value(const PromptKeys& src, const PromptSeq& seq, int b, int H, int head, int key) {
+  return prompt_row<D, PAGED>(src, src.V, src.ldv, seq, b, H, head, key);
+}
+
+struct PromptKernel {
+  const uint16_t* Q;
+  uint16_t* O;
+  PromptKeys src;
+  PromptItems items;
+  int64_t ldq, ldo;
+  float c;
+  int negate;
+};
+
+// exponent all ones: a number that is not finite
+template <typename Tag>
+__device__ __forceinline__ bool wild(uint32_t pair, int half) {
+  constexpr uint32_t E = __is_same(Tag, bf16_tag) ? 0x7f80u : 0x7c00u;
+  return ((pair >> (16 * half)) & E) == E;
+}
+
+// By one wavefront, for rows q0 + r of its 32 whose outputs are not finite (bits r of `bad`): where a value that is not finite was among those that its tiles hold (up to key
+// `held`; those from `there` on are key there - 1 again) and that the row does not see, the row is worked out again from the keys that it sees, one after the other
+// (attn_rows.h), and stored. Returns the bits of those rows. (An accident of one token costs the rows around it that, and no others.)
+template <typename Tag, int D, bool CAUSAL, bool PAGED>
+__device__ __forceinline__ uint32_t prompt_redo(const PromptKernel& p, const PromptSeq& seq, int b, int head, int q0, uint32_t bad, int held, int there) {
+  const int lane = threadIdx.x & 63, G = p.items.G, rows = seq.n * G;
+  uint32_t redo = 0;
+#pragma clang loop unroll(disable)
+  while (bad) {
+    const int r = __builtin_ctz(bad);
+    bad &= bad - 1;
+    if (q0 + r >= rows) break;
+    const int tok = uniform((q0 + r) / G), g = q0 + r - tok * G, end = CAUSAL ? seq.m - seq.n + 1 + tok : seq.m;
+    const int last = held < there ? held : there, first = held > there && end > there - 1 ? there - 1 : end;
+    bool found = false;
+#pragma clang loop unroll(disable)
+    for (int key = (first > 0 ? first : 0) + lane; key < last; key += 64) {
+      const uint16_t* v = prompt_value<D, PAGED>(p.src, seq, b, p.items.H, head, key);
+#pragma clang loop unroll(disable)
+      for (int d = 0; d < D; d += 2) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(v + d);
+        found |= wild<Tag>(w, 0) || wild<Tag>(w, 1);
+      }
+    }
+    if (!__any(found)) continue;
+    redo |= 1u << r;
+    const int64_t at = (int64_t)(head * G + g) * D;
+    const uint16_t* q = p.Q + (int64_t)(seq.q0 + tok) * p.ldq + at;
+    const float c = p.negate ? -p.c : p.c;
+    attend_row<Tag, D>(q, p.O + (int64_t)(seq.q0 + tok) * p.ldo + at, end, [&](int64_t j) { return prompt_key<D, PAGED>(p.src, seq, b, p.items.H, head, (int)j); },
+                       [&](int64_t j) { return prompt_value<D, PAGED>(p.src, seq, b, p.items.H, head, (int)j); }, c);
+  }
+  return redo;
+}
 
 }  // namespace mlt

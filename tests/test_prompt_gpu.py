@@ -97,10 +97,24 @@ def test_unseen_keys_have_no_influence(binding, dtype, D, bad):
             dirty[at] = bad
             O = binding.mlt_mha_packed_fwd(Q, dirty if which is K else K, dirty if which is V else V, ints(cu), ints(ku), scale)
             first = cu[b] + max(0, at - ku[b] - (batch[b][1] - batch[b][0]))         # the first query that sees it
-            assert torch.equal(O[:first], clean[:first]) and torch.equal(O[cu[b + 1]:], clean[cu[b + 1]:]), (at, which is K)
+            assert torch.equal(O[:cu[b]], clean[:cu[b]]) and torch.equal(O[cu[b + 1]:], clean[cu[b + 1]:]), (at, which is K)
+            n, m = first - cu[b], ku[b + 1] - ku[b] - (cu[b + 1] - first)            # the sequence as far as nothing has happened
+            check_packed(O[cu[b]:first], Q[cu[b]:first], K[ku[b]:ku[b] + m], V[ku[b]:ku[b] + m], [0, n], [0, m], scale, True, what="key %d" % at)
             if which is V:
                 want = torch.full_like(O[first:cu[b + 1]], bad)
                 assert torch.equal(O[first:cu[b + 1]].nan_to_num(9.0, 8.0, 7.0), want.nan_to_num(9.0, 8.0, 7.0)), (at, bad)
+
+
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+def test_an_infinity_in_the_last_value(binding, causal):
+    """Tiles that the keys do not fill repeat the last one: an infinity there is one in the output, not NaN."""
+    cu, ku, Q, K, V = make(8, [(3, 3), (50, 70), (1, 200)], 4, 2, 64, BF)
+    for b in range(3):
+        dirty = V.clone()
+        dirty[ku[b + 1] - 1] = -math.inf
+        O = binding.mlt_mha_packed_fwd(Q, K, dirty, ints(cu), ints(ku), 0.1, causal=causal)
+        assert bool(torch.isneginf(O[cu[b + 1] - 1 if causal else cu[b]:cu[b + 1]]).all())
+        assert int(torch.isfinite(O).all(-1).all(-1).sum()) == (cu[-1] - 1 if causal else cu[-1] - (cu[b + 1] - cu[b]))
 
 
 @pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
