@@ -69,7 +69,7 @@ def test_w4_refusals(b):
     _refuses(b, f, ok,
              [dict(dtype=2), dict(M=-1), dict(N=-1), dict(K=-32), dict(group=0), dict(A=None), dict(Wq=None), dict(S=None), dict(C=None), dict(lda=120), dict(ldw=48), dict(lds=7),
               dict(ldz=7), dict(ldc=7), dict(A=ODD), dict(Wq=ODD), dict(S=ctypes.c_void_p(0x10001)), dict(C=ctypes.c_void_p(0x10001))],
-             [dict(group=16), dict(group=256), dict(K=112), dict(lda=132), dict(ldw=72), dict(M=BIG), dict(N=BIG), dict(lda=1 << 26), dict(ldw=1 << 26)])
+             [dict(group=16), dict(group=256), dict(K=112), dict(lda=132), dict(ldw=72), dict(M=BIG), dict(N=BIG), dict(lda=1 << 26), dict(ldw=1 << 26), dict(lds=1 << 26), dict(ldz=1 << 26)])
     assert f(*_with(ok, M=0, A=None)) == b.MLT_OK and f(*_with(ok, N=0, C=None)) == b.MLT_OK
 
 
