@@ -112,6 +112,7 @@ class MltError(RuntimeError):
 # every call goes through the functions below.
 class _PythonOnly:
     gemm = gemm_acc = gemm_bias_act = mha_fwd = paged_attn_decode = quant_fp8 = gemm_fp8 = paged_append = paged_attn_decode_fp8 = staticmethod(lambda *args: None)
+    mha_packed_fwd = paged_attn_prompt = paged_attn_decode_prefix = gemm_w4 = gemm
 
 
 _fast = _PythonOnly
@@ -120,7 +121,7 @@ try:
     if _fastcall.torch_version == torch.__version__:
         _fastcall.bind(MltError, *(ctypes.cast(getattr(_lib, _f), _p).value for _f in (
             "mlt_gemm", "mlt_gemm_bias_act", "mlt_gemm_acc", "mlt_mha_fwd", "mlt_paged_attn_decode", "mlt_quant_fp8", "mlt_gemm_fp8", "mlt_paged_append",
-            "mlt_paged_append_fp8", "mlt_paged_attn_decode_fp8")))
+            "mlt_paged_append_fp8", "mlt_paged_attn_decode_fp8", "mlt_mha_packed_fwd", "mlt_paged_attn_prompt", "mlt_paged_attn_decode_prefix", "mlt_gemm_w4")))
         _fast = _fastcall
 except ImportError:
     pass
@@ -692,6 +693,9 @@ def mlt_mha_packed_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, q_offs
     name = "mlt_mha_packed_fwd"
     if k_offsets is None:
         k_offsets = q_offsets
+    done = _fast.mha_packed_fwd(Q, K, V, q_offsets, k_offsets, scale, causal, O, stream)
+    if done is not None:
+        return done
     _gpu(name, Q, K, V, q_offsets, k_offsets, O)
     dt, ldq, ldo, O = _packed_queries(name, Q, O, stream)
     T, Hq, D = Q.shape
@@ -716,6 +720,9 @@ def mlt_paged_attn_prompt(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, o
     block_size, D] with Hq a multiple of H; offsets int32 [B + 1]: the rows of each sequence; seq_lens int32 [B]: its tokens with the new ones;
     block_table int32 [B, max_blocks]. Returns O [T, Hq, D]; rows of no sequence are left as they are."""
     name = "mlt_paged_attn_prompt"
+    done = _fast.paged_attn_prompt(Q, Kc, Vc, offsets, seq_lens, block_table, scale, O, stream)
+    if done is not None:
+        return done
     _gpu(name, Q, Kc, Vc, offsets, seq_lens, block_table, O)
     dt, ldq, ldo, O = _packed_queries(name, Q, O, stream)
     T, Hq, D = Q.shape
@@ -747,6 +754,9 @@ def mlt_paged_attn_decode_prefix(Q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Te
     mlt_paged_append, the prefix's tokens among a sequence's. work: uint8, mlt_paged_attn_decode_prefix_work bytes, for calls that are captured into
     a graph. Returns O [B, Hq, D]."""
     name = "mlt_paged_attn_decode_prefix"
+    done = _fast.paged_attn_decode_prefix(Q, Kc, Vc, prefix_table, prefix_len, block_table, seq_lens, scale, O, work, stream)
+    if done is not None:
+        return done
     _gpu(name, Q, Kc, Vc, prefix_table, block_table, seq_lens, O, work)
     dt, P = _dtype_code(Q), int(prefix_len)
     if Q.dim() != 3:
@@ -783,6 +793,9 @@ def mlt_gemm_w4(A: torch.Tensor, Wq: torch.Tensor, S: torch.Tensor, Z: torch.Ten
     """C = A @ W.T with 4-bit weights: A [M, K]; Wq uint8 [N, K / 2], element k in the low (even k) or high half of byte k / 2; S [ceil(K / group), N] of
     A's type; Z uint8 [ceil(K / group), N] or None (8): W[n, k] = S[k // group, n] * (q[n, k] - Z[k // group, n]). Returns C [M, N]."""
     name = "mlt_gemm_w4"
+    done = _fast.gemm_w4(A, Wq, S, Z, group, C, stream)
+    if done is not None:
+        return done
     _gpu(name, A, Wq, S, Z, C)
     dt, g = _dtype_code(A), int(group)
     if Wq.dtype != torch.uint8 or (Z is not None and Z.dtype != torch.uint8) or S.dtype != A.dtype:

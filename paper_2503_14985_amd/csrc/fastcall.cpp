@@ -27,6 +27,10 @@ decltype(&mlt_gemm_fp8) call_gemm_fp8;
 decltype(&mlt_paged_append) call_append;
 decltype(&mlt_paged_append_fp8) call_append_fp8;
 decltype(&mlt_paged_attn_decode_fp8) call_paged_fp8;
+decltype(&mlt_mha_packed_fwd) call_packed;
+decltype(&mlt_paged_attn_prompt) call_prompt;
+decltype(&mlt_paged_attn_decode_prefix) call_prefix;
+decltype(&mlt_gemm_w4) call_gemm_w4;
 PyObject* error_class;      // binding.MltError(status, where)
 
 // A plain tensor with memory of its own kind on GPU `device` (-1: the first one sets it), or null
@@ -335,6 +339,134 @@ PyObject* py_paged_fp8(PyObject*, PyObject* const* v, Py_ssize_t n) {
   return result(rc, v[8], "mlt_paged_attn_decode_fp8");
 }
 
+// ---- prompts, shared prefixes, 4-bit weights
+
+// int32 and contiguous, of one dimension of n elements (n < 0: any number)
+bool numbers(const at::Tensor& t, int64_t n) { return is(t, at::kInt) && t.dim() == 1 && (n < 0 || t.size(0) == n) && t.is_contiguous(); }
+// a 16-bit paged cache for heads of D
+bool paged_cache(const at::Tensor& kc, const at::Tensor& vc, at::ScalarType type, int64_t D) {
+  return is(kc, type) && is(vc, type) && kc.dim() == 4 && kc.size(3) == D && vc.sizes() == kc.sizes() && kc.is_contiguous() && vc.is_contiguous();
+}
+
+// mha_packed_fwd(Q, K, V, q_offsets, k_offsets, scale, causal, O, stream)
+PyObject* py_packed(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 9 || v[8] != Py_None || !PyFloat_CheckExact(v[5]) || !PyBool_Check(v[6])) Py_RETURN_NONE;
+  int device = -1;
+  const at::Tensor* t[6];
+  PyObject* const o[6] = {v[0], v[1], v[2], v[3], v[4], v[7]};
+  for (int i = 0; i < 6; ++i)
+    if (!(t[i] = plain(o[i], device))) Py_RETURN_NONE;
+  const at::Tensor &q = *t[0], &k = *t[1], &vv = *t[2], &qo = *t[3], &ko = *t[4], &out = *t[5];
+  const int dtype = dtype_code(q);
+  if (dtype < 0 || q.dim() != 3 || k.dim() != 3 || !is(k, q.scalar_type()) || !is(vv, q.scalar_type()) || !is(out, q.scalar_type())) Py_RETURN_NONE;
+  const int64_t T = q.size(0), Hq = q.size(1), D = q.size(2), Tk = k.size(0), H = k.size(1);
+  if (k.size(2) != D || vv.sizes() != k.sizes() || out.sizes() != q.sizes()) Py_RETURN_NONE;
+  const int64_t ldq = head_rows(q, T, D), ldk = head_rows(k, Tk, D), ldv = head_rows(vv, Tk, D), ldo = head_rows(out, T, D);
+  if (ldq < 0 || ldk < 0 || ldv < 0 || ldo < 0 || !numbers(qo, -1) || !numbers(ko, qo.size(0)) || qo.size(0) < 1) Py_RETURN_NONE;
+  void* stream;
+  if (!on_current_device(device, &stream)) Py_RETURN_NONE;
+  void* p[6];
+  for (int i = 0; i < 6; ++i) p[i] = t[i]->data_ptr();
+  const int64_t B = qo.size(0) - 1;
+  const float scale = (float)PyFloat_AS_DOUBLE(v[5]);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = call_packed(T, Tk, B, Hq, H, D, p[0], ldq, p[1], ldk, p[2], ldv, (const int32_t*)p[3], (const int32_t*)p[4], p[5], ldo, scale, v[6] == Py_True, dtype, stream);
+  Py_END_ALLOW_THREADS
+  return result(rc, v[7], "mlt_mha_packed_fwd");
+}
+
+// paged_attn_prompt(Q, Kc, Vc, offsets, seq_lens, block_table, scale, O, stream)
+PyObject* py_prompt(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 9 || v[8] != Py_None || !PyFloat_CheckExact(v[6])) Py_RETURN_NONE;
+  int device = -1;
+  const at::Tensor* t[7];
+  PyObject* const o[7] = {v[0], v[1], v[2], v[3], v[4], v[5], v[7]};
+  for (int i = 0; i < 7; ++i)
+    if (!(t[i] = plain(o[i], device))) Py_RETURN_NONE;
+  const at::Tensor &q = *t[0], &kc = *t[1], &vc = *t[2], &off = *t[3], &lens = *t[4], &table = *t[5], &out = *t[6];
+  const int dtype = dtype_code(q);
+  if (dtype < 0 || q.dim() != 3 || !is(out, q.scalar_type()) || out.sizes() != q.sizes()) Py_RETURN_NONE;
+  const int64_t T = q.size(0), Hq = q.size(1), D = q.size(2);
+  const int64_t ldq = head_rows(q, T, D), ldo = head_rows(out, T, D);
+  if (ldq < 0 || ldo < 0 || !paged_cache(kc, vc, q.scalar_type(), D) || !numbers(lens, -1)) Py_RETURN_NONE;
+  const int64_t B = lens.size(0);
+  if (!numbers(off, B + 1) || !is(table, at::kInt) || table.dim() != 2 || table.size(0) != B || !table.is_contiguous()) Py_RETURN_NONE;
+  void* stream;
+  if (!on_current_device(device, &stream)) Py_RETURN_NONE;
+  void* p[7];
+  for (int i = 0; i < 7; ++i) p[i] = t[i]->data_ptr();
+  const int64_t nb = kc.size(0), H = kc.size(1), bs = kc.size(2), per = table.size(1);
+  const float scale = (float)PyFloat_AS_DOUBLE(v[6]);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = call_prompt(T, B, Hq, H, D, bs, per, nb, p[0], ldq, p[1], p[2], (const int32_t*)p[3], (const int32_t*)p[4], (const int32_t*)p[5], p[6], ldo, scale, dtype, stream);
+  Py_END_ALLOW_THREADS
+  return result(rc, v[7], "mlt_paged_attn_prompt");
+}
+
+// paged_attn_decode_prefix(Q, Kc, Vc, prefix_table, prefix_len, block_table, seq_lens, scale, O, work, stream), work or None
+PyObject* py_prefix(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 11 || v[10] != Py_None || !PyLong_CheckExact(v[4]) || !PyFloat_CheckExact(v[7])) Py_RETURN_NONE;
+  int overflow = 0, device = -1;
+  const long long P = PyLong_AsLongLongAndOverflow(v[4], &overflow);
+  if (overflow || P < 0) Py_RETURN_NONE;
+  const at::Tensor* t[8] = {};
+  PyObject* const o[8] = {v[0], v[1], v[2], v[3], v[5], v[6], v[8], v[9]};
+  for (int i = 0; i < 8; ++i) {
+    if (i == 7 && v[9] == Py_None) continue;
+    if (!(t[i] = plain(o[i], device)) || !t[i]->is_contiguous()) Py_RETURN_NONE;
+  }
+  const at::Tensor &q = *t[0], &kc = *t[1], &vc = *t[2], &pre = *t[3], &table = *t[4], &lens = *t[5], &out = *t[6];
+  const int dtype = dtype_code(q);
+  if (dtype < 0 || q.dim() != 3 || !is(out, q.scalar_type()) || out.sizes() != q.sizes()) Py_RETURN_NONE;
+  const int64_t B = q.size(0), Hq = q.size(1), D = q.size(2);
+  if (!paged_cache(kc, vc, q.scalar_type(), D) || !numbers(lens, B) || !numbers(pre, -1)) Py_RETURN_NONE;
+  const int64_t nb = kc.size(0), H = kc.size(1), bs = kc.size(2);
+  if (!is(table, at::kInt) || table.dim() != 2 || table.size(0) != B || pre.size(0) * bs < P || (t[7] && !is(*t[7], at::kByte))) Py_RETURN_NONE;
+  void* stream;
+  if (!on_current_device(device, &stream)) Py_RETURN_NONE;
+  void* p[8];
+  for (int i = 0; i < 8; ++i) p[i] = t[i] ? t[i]->data_ptr() : nullptr;
+  const int64_t per = table.size(1), bytes = t[7] ? t[7]->numel() : 0;
+  const float scale = (float)PyFloat_AS_DOUBLE(v[7]);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = call_prefix(B, Hq, H, D, bs, per, nb, p[0], p[1], p[2], (const int32_t*)p[3], P, (const int32_t*)p[4], (const int32_t*)p[5], p[6], scale, p[7], bytes, dtype, stream);
+  Py_END_ALLOW_THREADS
+  return result(rc, v[8], "mlt_paged_attn_decode_prefix");
+}
+
+// gemm_w4(A, Wq, S, Z, group, C, stream), Z or None
+PyObject* py_gemm_w4(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (n != 7 || v[6] != Py_None || !PyLong_CheckExact(v[4])) Py_RETURN_NONE;
+  int overflow = 0, device = -1;
+  const long group = PyLong_AsLongAndOverflow(v[4], &overflow);
+  if (overflow || group < 1) Py_RETURN_NONE;
+  const at::Tensor* t[5] = {};
+  int64_t ld[5] = {};
+  PyObject* const o[5] = {v[0], v[1], v[2], v[3], v[5]};
+  for (int i = 0; i < 5; ++i) {
+    if (i == 3 && v[3] == Py_None) continue;
+    if (!(t[i] = plain(o[i], device)) || (ld[i] = row_stride(*t[i])) < 0) Py_RETURN_NONE;
+  }
+  const at::Tensor &a = *t[0], &w = *t[1], &s = *t[2], &c = *t[4];
+  const int dtype = dtype_code(a);
+  if (dtype < 0 || !is(w, at::kByte) || !is(s, a.scalar_type()) || !is(c, a.scalar_type())) Py_RETURN_NONE;
+  const int64_t M = a.size(0), K = a.size(1), N = w.size(0), groups = (K + group - 1) / group;
+  if (2 * w.size(1) != K || !sized(s, groups, N) || !sized(c, M, N)) Py_RETURN_NONE;
+  if (t[3] && (!is(*t[3], at::kByte) || !sized(*t[3], groups, N))) Py_RETURN_NONE;
+  void* stream;
+  if (!on_current_device(device, &stream)) Py_RETURN_NONE;
+  void* p[5];
+  for (int i = 0; i < 5; ++i) p[i] = t[i] ? t[i]->data_ptr() : nullptr;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = call_gemm_w4(M, N, K, p[0], ld[0], p[1], ld[1], group, p[2], ld[2], (const uint8_t*)p[3], ld[3], p[4], ld[4], dtype, stream);
+  Py_END_ALLOW_THREADS
+  return result(rc, v[5], "mlt_gemm_w4");
+}
+
 // A torch error in here (a tensor without memory behind it, say) is binding.py's to meet again
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* v, Py_ssize_t n) {
@@ -347,11 +479,12 @@ PyObject* guarded(PyObject* self, PyObject* const* v, Py_ssize_t n) {
 }
 
 // bind(error class, gemm, gemm_bias_act, gemm_acc, mha_fwd, paged_attn_decode[, quant_fp8, gemm_fp8, paged_append, paged_append_fp8,
-// paged_attn_decode_fp8]): the library functions' addresses; those that are left out stay as they are
+// paged_attn_decode_fp8[, mha_packed_fwd, paged_attn_prompt, paged_attn_decode_prefix, gemm_w4]]): the library functions' addresses; those that are left out
+// stay as they are
 PyObject* py_bind(PyObject*, PyObject* args) {
-  Py_ssize_t a[10] = {};
+  Py_ssize_t a[14] = {};
   PyObject* err;
-  if (!PyArg_ParseTuple(args, "Onnnnn|nnnnn", &err, &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &a[9])) return nullptr;
+  if (!PyArg_ParseTuple(args, "Onnnnn|nnnnnnnnn", &err, &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &a[9], &a[10], &a[11], &a[12], &a[13])) return nullptr;
   Py_INCREF(err);
   error_class = err;
   call_gemm = reinterpret_cast<decltype(call_gemm)>(a[0]);
@@ -364,6 +497,10 @@ PyObject* py_bind(PyObject*, PyObject* args) {
   if (a[7]) call_append = reinterpret_cast<decltype(call_append)>(a[7]);
   if (a[8]) call_append_fp8 = reinterpret_cast<decltype(call_append_fp8)>(a[8]);
   if (a[9]) call_paged_fp8 = reinterpret_cast<decltype(call_paged_fp8)>(a[9]);
+  if (a[10]) call_packed = reinterpret_cast<decltype(call_packed)>(a[10]);
+  if (a[11]) call_prompt = reinterpret_cast<decltype(call_prompt)>(a[11]);
+  if (a[12]) call_prefix = reinterpret_cast<decltype(call_prefix)>(a[12]);
+  if (a[13]) call_gemm_w4 = reinterpret_cast<decltype(call_gemm_w4)>(a[13]);
   Py_RETURN_NONE;
 }
 
@@ -377,6 +514,10 @@ PyMethodDef methods[] = {MLT_FAST("gemm", py_gemm),
                          MLT_FAST("gemm_fp8", py_gemm_fp8),
                          MLT_FAST("paged_append", py_append),
                          MLT_FAST("paged_attn_decode_fp8", py_paged_fp8),
+                         MLT_FAST("mha_packed_fwd", py_packed),
+                         MLT_FAST("paged_attn_prompt", py_prompt),
+                         MLT_FAST("paged_attn_decode_prefix", py_prefix),
+                         MLT_FAST("gemm_w4", py_gemm_w4),
                          {"bind", py_bind, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
