@@ -22,8 +22,8 @@ namespace mlt {
 
 namespace {
 
-constexpr int W4_NW = 8, W4_NT = W4_NW * 64;
-constexpr int W4_RING = 19 * 1024 + 512;   // LDS ring of a wavefront: 156 KB in all
+constexpr int W4_RING = 19 * 1024 + 512;   // LDS ring of a wavefront of eight: 156 KB in all
+constexpr int W4_GB = 8;                   // blocks of 16 columns whose sums are kept at once
 constexpr int W4_ROWS = 64;                // rows of C of a workgroup
 
 // a 16-bit (8-bit) number for each lane (uniform base + per-lane byte offset), as a dword to lds_addr + 4 * lane
@@ -34,16 +34,15 @@ __device__ __forceinline__ void load_lds_u8(const void* base, uint32_t voff, uin
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2" : : "s"(lds_addr), "v"(voff), "s"(base) : "memory", "m0");
 }
 
-// 16 + q of nibbles i and i + 4
-template <typename Tag> __device__ __forceinline__ uint32_t nibbles(uint32_t w, int i) {
-  if constexpr (__is_same(Tag, bf16_tag)) {
-    const uint32_t x = i == 0 ? w << 3 : w >> (4 * i - 3);
-    return (x & 0x00780078u) | 0x41804180u;
-  } else {
-    const uint32_t x = i < 2 ? w << (6 - 4 * i) : w >> (4 * i - 6);
-    return (x & 0x03c003c0u) | 0x4c004c00u;
+// 16 + q of nibbles i and i + 4. The two constants are given in registers: and-or takes no two literals.
+template <typename Tag> struct Nibbles {
+  static constexpr bool BF = __is_same(Tag, bf16_tag);
+  static constexpr uint32_t MASK = BF ? 0x00780078u : 0x03c003c0u, SIXTEEN = BF ? 0x41804180u : 0x4c004c00u;
+  static __device__ __forceinline__ uint32_t get(uint32_t w, int i, uint32_t mask, uint32_t sixteen) {
+    const int right = 4 * i - (BF ? 3 : 6);
+    return ((right < 0 ? w << -right : w >> right) & mask) | sixteen;
   }
-}
+};
 
 struct W4 {
   int M, N, K, share, rest, lda, ldw;
@@ -58,19 +57,20 @@ struct W4 {
   uint32_t* counter;
 };
 
-// MT: 16-row tiles of A; G: group; KP: k of a piece; GB: blocks of columns in a group of blocks, at most
-template <typename Tag, int MT, int G, int KP, int GB>
-__global__ __launch_bounds__(W4_NT, 2) void gemm_4bit_kernel(W4 a) {
+// MT: 16-row tiles of A; G: group; KP: k of a piece; NW: wavefronts; ZP: with zero points
+template <typename Tag, int MT, int G, int KP, int NW, bool ZP>
+__global__ __launch_bounds__(NW * 64, NW / 4) void gemm_4bit_kernel(W4 a) {
   typedef typename Elem<Tag>::vec8 V8;
+  constexpr int GB = W4_GB, NT = NW * 64;
+  constexpr int RING = 8 * W4_RING / NW;                   // LDS ring of a wavefront
   constexpr int NS = KP / 32, NG = KP / G, SPG = G / 32;   // steps and groups of a piece, steps of a group
   constexpr int AROW = KP * 2, WROW = KP / 2;              // bytes of a row
-  constexpr int ARI = 1024 / AROW, WRI = 1024 / WROW;      // rows of a load: 1 or 2, 4 or 8
+  constexpr int ARI = 1024 / AROW, WRI = 1024 / WROW;      // rows of a load
   constexpr int BODY = 4 * AROW, NL = BODY / 1024;         // a slot holds 4 rows of A or 16 of W: loads of it
   constexpr int NSL = (NG * 16 + 63) / 64;                 // loads of a block's scales, of its zero points
-  constexpr int SIDE = NSL * 256;
+  constexpr int SIDE = NSL * 256, SLOT = BODY + SIDE * (ZP ? 2 : 1), SLOTS = RING / SLOT, W_LOADS = NL + NSL * (ZP ? 2 : 1);
+  constexpr bool WHOLE = SLOTS >= 5;                       // room for a tile of A and more
   static_assert(BODY == 16 * WROW, "one size for both");
-  constexpr bool WHOLE = KP == 256;
-  static_assert(!WHOLE || W4_RING / (BODY + 2 * SIDE) >= 4, "room for a tile of A");
   static_assert(WHOLE || MT == 1, "a tile of A slot by slot: its zeros and sums are those of the last one");
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -87,31 +87,37 @@ __global__ __launch_bounds__(W4_NT, 2) void gemm_4bit_kernel(W4 a) {
     p0 = part_id * per;
     p1 = p0 + per < all ? p0 + per : all;
   }
-  const int first = p0 + wave, mine = p1 > first ? (p1 - first + W4_NW - 1) / W4_NW : 0;
+  const int first = p0 + wave, mine = p1 > first ? (p1 - first + NW - 1) / NW : 0;
+  // A wavefront begins somewhere in its share and goes round, so that the workgroups are not all at the same place of the rows, which are a power of two apart more often than
+  // not: that would be the same few memory channels.
+  const int start = mine > 0 ? first + (wave + bid) % mine * NW : first;
   const int last_group = (K - 1) / G;
-  const int slot_bytes = BODY + SIDE * (a.Z ? 2 : 1), slots = W4_RING / slot_bytes;
-  const uint32_t ring = (uint32_t)(uintptr_t)(lptr_t)smem + (uint32_t)wave * W4_RING, ring_end = ring + slots * slot_bytes;
+  const uint32_t ring = (uint32_t)(uintptr_t)(lptr_t)smem + (uint32_t)wave * RING, ring_end = ring + SLOTS * SLOT;
   const int SA = (M + 3) / 4;                              // slots of A
 
   // A: row 4 i + n of slot i is row n of it, chunk c (8 k) at position c ^ row (low four bits); W: chunk c (32 k) of row n at position c ^ f(n)
   constexpr int ACH = AROW / 16, WCH = WROW / 16;
-  auto fw = [](int n) { return WCH == 16 ? n : (n >> 1) & 7; };
+  auto fw = [](int n) { return WCH == 16 ? n : WCH == 8 ? (n >> 1) & 7 : (n >> 2) & 3; };
   auto side_group = [](int i, int ln) { const int q = (i * 64 + ln) >> 4; return q < NG ? q : NG - 1; };   // a lane's group of the piece (lanes to spare: the last one)
-  // per-lane byte offsets of the loads of a slot of W, of its scales and zero points, where all of them are there
-  uint32_t vw[NL], vs[NSL];
+  // per-lane byte offsets of the loads of a slot of W, of its scales and zero points, where all of them are there; and of one of A (its row of the load)
+  uint32_t vw[NL], vs[NSL], vz[ZP ? NSL : 1];
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
     const int row = i * WRI + lane / WCH;
     vw[i] = (uint32_t)row * (uint32_t)a.ldw + (uint32_t)((lane % WCH) ^ fw(row)) * 16u;
   }
 #pragma unroll
-  for (int i = 0; i < NSL; ++i) vs[i] = (uint32_t)side_group(i, lane) * (uint32_t)a.lds + (uint32_t)(lane & 15);   // (in numbers)
+  for (int i = 0; i < NSL; ++i) {
+    vs[i] = ((uint32_t)side_group(i, lane) * (uint32_t)a.lds + (uint32_t)(lane & 15)) * 2u;
+    if (ZP) vz[i] = (uint32_t)side_group(i, lane) * (uint32_t)a.ldz + (uint32_t)(lane & 15);
+  }
+  const int a_in = lane / ACH;
+  const uint32_t a_row = (uint32_t)a_in * (uint32_t)a.lda * 2u, a_chunk = (uint32_t)(((lane % ACH) ^ a_in) * 16);
   // this lane's places in a slot of A (its chunk 4 s + g by XOR, slots begin on 256 bytes) and of W (its word of chunk s)
   const uint32_t a_lane = (uint32_t)((r16 & 3) * AROW + ((g ^ r16) << 4)), w_lane = (uint32_t)(r16 * WROW + (fw(r16) << 4) + 4 * g);
-  // without zero points the scales are read in their place, and multiplied by 0
-  const uint32_t z_at = a.Z ? SIDE : 0;
-  const float z_mul = a.Z ? -1.f : 0.f, z_add = a.Z ? -16.f : -24.f;
-  static_assert(W4_RING % 256 == 0 && SIDE % 256 == 0 && BODY % 256 == 0, "...");
+  static_assert(RING % 256 == 0 && SLOT % 256 == 0 && W4_RING % 256 == 0, "see a_lane");
+  uint32_t mask = Nibbles<Tag>::MASK, sixteen = Nibbles<Tag>::SIXTEEN;
+  asm volatile("" : "+v"(mask), "+v"(sixteen));
 
   for (int base = 0; base < nblk; base += GB) {
     const int nb = nblk - base < GB ? nblk - base : GB;
@@ -122,37 +128,44 @@ __global__ __launch_bounds__(W4_NT, 2) void gemm_4bit_kernel(W4 a) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) acc[b][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // the cursor: the next slot of the stream to fetch, f_s of piece f_p, and its place
-    int f_t = 0, f_s = 0, f_p = first, issued = 0, need = 0;
+    // the cursor: the next slot of the stream to fetch, f_s of piece f_p, where its rows begin, and its place
+    int f_t = 0, f_s = 0, f_p = start, f_rows = 0, issued = 0, need = 0;
     uint32_t f_slot = ring;
+    const uint16_t *f_a = nullptr, *f_sc = nullptr;
+    const uint8_t *f_w = nullptr, *f_z = nullptr;
+    auto piece_begins = [&]() __attribute__((always_inline)) {
+      const int k0 = f_p * KP;
+      f_a = A + k0;
+      f_rows = M;
+      f_w = a.W + (int64_t)(c0 + base * 16) * a.ldw + k0 / 2;
+      f_sc = a.S + k0 / G * a.lds + c0 + base * 16;
+      if (ZP) f_z = a.Z + k0 / G * a.ldz + c0 + base * 16;
+    };
+    if (T > 0) piece_begins();
     auto fetch = [&]() __attribute__((always_inline)) {
       if (f_t >= T) return;
       const int k0 = f_p * KP;
       const bool tail = k0 + KP > K;                       // chunks past K: the row's first one; they count as zeros
       if (f_s < SA) {
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-          const int row = f_s * 4 + i * ARI;               // (uniform; with two rows a load the second may be one too many: the first again)
-          if (row < M) {
-            const int in = ARI == 1 ? 0 : lane / ACH;
-            int c = (lane % ACH) ^ ((row & 15) + in);
-            if (tail && k0 + c * 8 >= K) c = 0;
-            load_lds16(A + (int64_t)row * a.lda + k0, (ARI > 1 && in && row + 1 < M ? (uint32_t)a.lda * 2u : 0u) + (uint32_t)c * 16u, f_slot + i * 1024u);
+        for (int i = 0; i < NL; ++i)
+          if (i * ARI < f_rows) {                          // (with several rows a load the last ones may be too many: the first again)
+            uint32_t c = a_chunk ^ (uint32_t)(((f_s & 3) * 4 + i * ARI) << 4);
+            if (tail && k0 * 2 + (int)c >= K * 2) c = 0;
+            load_lds16(f_a + (int64_t)(i * ARI) * a.lda, (ARI > 1 && i * ARI + a_in < f_rows ? a_row : 0u) + c, f_slot + i * 1024u);
             ++issued;
           }
-        }
+        f_a += 4 * (int64_t)a.lda;
+        f_rows -= 4;
       } else {
-        const int n0 = c0 + (base + f_s - SA) * 16, rows = c1 - n0, g0 = k0 / G;
-        const uint8_t* src = a.W + (int64_t)n0 * a.ldw + k0 / 2;
-        const uint16_t* sp = a.S + g0 * a.lds + n0;
-        const uint8_t* zp = a.Z + g0 * a.ldz + n0;
-        if (!tail && rows >= 16) {
+        if (f_s == SA) f_rows = c1 - (c0 + base * 16);
+        if (!tail && f_rows >= 16) {
 #pragma unroll
-          for (int i = 0; i < NL; ++i) load_lds16_stream(src, vw[i], f_slot + i * 1024u);
+          for (int i = 0; i < NL; ++i) load_lds16_stream(f_w, vw[i], f_slot + i * 1024u);
 #pragma unroll
           for (int i = 0; i < NSL; ++i) {
-            load_lds_u16(sp, vs[i] * 2u, f_slot + BODY + i * 256u);
-            if (a.Z) load_lds_u8(zp, vs[i] + (uint32_t)side_group(i, lane) * (uint32_t)(a.ldz - a.lds), f_slot + BODY + SIDE + i * 256u);
+            load_lds_u16(f_sc, vs[i], f_slot + BODY + i * 256u);
+            if (ZP) load_lds_u8(f_z, vz[i], f_slot + BODY + SIDE + i * 256u);
           }
         } else {                                           // columns that are not there: the first one's weights, the last one's scales; groups: the last one's
           int ln = lane;
@@ -160,29 +173,34 @@ __global__ __launch_bounds__(W4_NT, 2) void gemm_4bit_kernel(W4 a) {
 #pragma unroll
           for (int i = 0; i < NL; ++i) {
             const int row = i * WRI + ln / WCH, c = (ln % WCH) ^ fw(row);
-            load_lds16_stream(src, row < rows && k0 + c * 32 < K ? (uint32_t)row * (uint32_t)a.ldw + (uint32_t)c * 16u : 0u, f_slot + i * 1024u);
+            load_lds16_stream(f_w, row < f_rows && k0 + c * 32 < K ? (uint32_t)row * (uint32_t)a.ldw + (uint32_t)c * 16u : 0u, f_slot + i * 1024u);
           }
 #pragma unroll
           for (int i = 0; i < NSL; ++i) {
-            const int n = (ln & 15) < rows ? ln & 15 : rows - 1, qq = side_group(i, ln), q = qq < last_group - g0 ? qq : last_group - g0;
-            load_lds_u16(sp, ((uint32_t)q * (uint32_t)a.lds + n) * 2u, f_slot + BODY + i * 256u);
-            if (a.Z) load_lds_u8(zp, (uint32_t)q * (uint32_t)a.ldz + n, f_slot + BODY + SIDE + i * 256u);
+            const int n = (ln & 15) < f_rows ? ln & 15 : f_rows - 1, most = last_group - k0 / G, q = side_group(i, ln) < most ? side_group(i, ln) : most;
+            load_lds_u16(f_sc, ((uint32_t)q * (uint32_t)a.lds + n) * 2u, f_slot + BODY + i * 256u);
+            if (ZP) load_lds_u8(f_z, (uint32_t)q * (uint32_t)a.ldz + n, f_slot + BODY + SIDE + i * 256u);
           }
         }
-        issued += a.Z ? NL + 2 * NSL : NL + NSL;
+        issued += W_LOADS;
+        f_w += 16 * (int64_t)a.ldw;
+        f_sc += 16;
+        if (ZP) f_z += 16;
+        f_rows -= 16;
       }
       ++f_t;
-      f_slot += slot_bytes;
+      f_slot += SLOT;
       if (f_slot == ring_end) f_slot = ring;
       if (++f_s == S) {
         f_s = 0;
-        f_p += W4_NW;
+        f_p = f_p + NW < p1 ? f_p + NW : first;
+        piece_begins();
       }
     };
 #pragma clang loop unroll(disable)
-    for (int i = 0; i < slots; ++i) fetch();
+    for (int i = 0; i < SLOTS; ++i) fetch();
 
-    // waits until the next `take` slots, of so many loads, have landed (what was issued after them may be in flight), and gives their places to the next ones
+    // waits until the next slots, of so many loads, have landed (what was issued after them may be in flight)
     uint32_t slot = ring;
     auto wait = [&](int loads) __attribute__((always_inline)) {
       need += loads;
@@ -190,27 +208,27 @@ __global__ __launch_bounds__(W4_NT, 2) void gemm_4bit_kernel(W4 a) {
 #ifdef MLT_DEBUG_BARRIERS
       later = 0;                                           // waits for all of them, so that a count that is too lax shows
 #endif
-      if (later >= 16) __builtin_amdgcn_s_waitcnt(wait_imm(16, 15));
-      else if (later >= 12) __builtin_amdgcn_s_waitcnt(wait_imm(12, 15));
-      else if (later >= 9) __builtin_amdgcn_s_waitcnt(wait_imm(9, 15));
-      else if (later >= 6) __builtin_amdgcn_s_waitcnt(wait_imm(6, 15));
-      else if (later >= 4) __builtin_amdgcn_s_waitcnt(wait_imm(4, 15));
+      constexpr int FULL = (SLOTS - 1) * W_LOADS < 63 ? (SLOTS - 1) * W_LOADS : 63;   // (the weights' steady state)
+      if (later >= FULL) __builtin_amdgcn_s_waitcnt(wait_imm(FULL, 15));
+      else if (later >= FULL * 2 / 3) __builtin_amdgcn_s_waitcnt(wait_imm(FULL * 2 / 3, 15));
+      else if (later >= 10) __builtin_amdgcn_s_waitcnt(wait_imm(10, 15));
+      else if (later >= 5) __builtin_amdgcn_s_waitcnt(wait_imm(5, 15));
       else if (later >= 2) __builtin_amdgcn_s_waitcnt(wait_imm(2, 15));
       else __builtin_amdgcn_s_waitcnt(wait_imm(0, 15));
       __builtin_amdgcn_sched_barrier(0);
     };
-    auto refill = [&](int take) __attribute__((always_inline)) {
-      __builtin_amdgcn_s_waitcnt(wait_imm(63, 0));         // (what was read has arrived)
+    auto refill = [&](int take) __attribute__((always_inline)) {   // the places of so many slots, which have been read, take the next ones
+      __builtin_amdgcn_s_waitcnt(wait_imm(63, 0));
       __builtin_amdgcn_sched_barrier(0);
 #pragma clang loop unroll(disable)
       for (int x = 0; x < take; ++x) {
         fetch();
         __builtin_amdgcn_sched_barrier(0);
-        slot += slot_bytes;
+        slot += SLOT;
         if (slot == ring_end) slot = ring;
       }
     };
-    for (int i = 0, piece = first; i < mine; ++i, piece += W4_NW) {
+    for (int i = 0, piece = start; i < mine; ++i, piece = piece + NW < p1 ? piece + NW : first) {
       const int k0 = piece * KP;
       const bool tail = k0 + KP > K;
       // ---- A: this lane's row r16 of each tile, step s: chunk 4 s + g; and its sums over the groups
@@ -222,16 +240,16 @@ __global__ __launch_bounds__(W4_NT, 2) void gemm_4bit_kernel(W4 a) {
         for (int s = 0; s < NS; ++s) af[mt][s] = u32x4{0u, 0u, 0u, 0u};
         const int rows = M - mt * 16 < 16 ? M - mt * 16 : 16;
         if (rows > 0) {
-          if (WHOLE) {                                     // the ring has room for the tile: each lane reads from its row's slot
+          if (WHOLE) {                                     // each lane reads from its row's slot
             const int take = (rows + 3) / 4;
             wait((rows + ARI - 1) / ARI);
-            const uint32_t at = slot + (uint32_t)(r16 < rows ? r16 >> 2 : 0) * (uint32_t)slot_bytes, from = (at >= ring_end ? at - (uint32_t)(slots * slot_bytes) : at) + a_lane;
+            const uint32_t at = slot + (uint32_t)(r16 < rows ? r16 >> 2 : 0) * (uint32_t)SLOT, from = (at >= ring_end ? at - (uint32_t)(SLOTS * SLOT) : at) + a_lane;
 #pragma unroll
             for (int s = 0; s < NS; ++s) af[mt][s] = *(const MLT_LDS u32x4*)(uintptr_t)((from ^ (uint32_t)((s & 3) << 6)) + (uint32_t)((s >> 2) * 256));
             refill(take);
           } else {                                         // slot by slot
             for (int q = 0; q * 4 < rows; ++q) {
-              wait(rows - q * 4 < 4 ? rows - q * 4 : 4);
+              wait((rows - q * 4 < 4 ? rows - q * 4 + ARI - 1 : 4) / ARI);
               if ((r16 >> 2) == q) {
 #pragma unroll
                 for (int s = 0; s < NS; ++s) af[mt][s] = *(const MLT_LDS u32x4*)(uintptr_t)(((slot + a_lane) ^ (uint32_t)((s & 3) << 6)) + (uint32_t)((s >> 2) * 256));
@@ -254,14 +272,14 @@ __global__ __launch_bounds__(W4_NT, 2) void gemm_4bit_kernel(W4 a) {
           f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int s = 0; s < SPG; ++s) sum = mfma16(__builtin_bit_cast(V8, u32x4{one, one, one, one}), __builtin_bit_cast(V8, af[mt][q * SPG + s]), sum);
-          sa[mt][q] = sum[0];
+          sa[mt][q] = ZP ? sum[0] : -24.f * sum[0];        // (without zero points: what is to be added)
           asm volatile("" : "+v"(sa[mt][q]));              // (a register of its own: the other three of the four are not to be kept with it)
           __builtin_amdgcn_sched_barrier(0);
         }
       }
 #pragma clang loop unroll(disable)
       for (int blk = 0; blk < nb; ++blk) {
-        wait(a.Z ? NL + 2 * NSL : NL + NSL);
+        wait(W_LOADS);
         // ---- a block of 16 columns: lane's column r16, step s: word 4 s + g. A group at a time, the next one's numbers read beside this one's products
         uint32_t w[2][SPG];
         u32x4 sc[2], zp[2];                                // scales and zero points of columns 4 g .. 4 g + 3
@@ -272,7 +290,7 @@ __global__ __launch_bounds__(W4_NT, 2) void gemm_4bit_kernel(W4 a) {
 #pragma unroll
           for (int s = 0; s < SPG; ++s) w[q & 1][s] = *(const MLT_LDS uint32_t*)(uintptr_t)((slot + w_lane) ^ (uint32_t)((q * SPG + s) << 4));
           sc[q & 1] = *(const MLT_LDS u32x4*)(uintptr_t)(slot + BODY + q * 64u + g * 16u);
-          zp[q & 1] = *(const MLT_LDS u32x4*)(uintptr_t)(slot + BODY + z_at + q * 64u + g * 16u);
+          if (ZP) zp[q & 1] = *(const MLT_LDS u32x4*)(uintptr_t)(slot + BODY + SIDE + q * 64u + g * 16u);
         };
         read(0);
 #pragma unroll
@@ -280,49 +298,57 @@ __global__ __launch_bounds__(W4_NT, 2) void gemm_4bit_kernel(W4 a) {
           if (q + 1 < NG) read(q + 1);
           f32x4 sum[MT];
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt) sum[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int mt = 0; mt < MT; ++mt) sum[mt] = ZP ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{sa[mt][q], sa[mt][q], sa[mt][q], sa[mt][q]};
 #pragma unroll
           for (int s = 0; s < SPG; ++s) {
             const uint32_t x = w[q & 1][s];
-            const u32x4 wf = {nibbles<Tag>(x, 0), nibbles<Tag>(x, 1), nibbles<Tag>(x, 2), nibbles<Tag>(x, 3)};
+            const u32x4 wf = {Nibbles<Tag>::get(x, 0, mask, sixteen), Nibbles<Tag>::get(x, 1, mask, sixteen), Nibbles<Tag>::get(x, 2, mask, sixteen), Nibbles<Tag>::get(x, 3, mask, sixteen)};
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) sum[mt] = mfma16(__builtin_bit_cast(V8, wf), __builtin_bit_cast(V8, af[mt][q * SPG + s]), sum[mt]);
           }
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float scale = Elem<Tag>::to_f32((uint16_t)sc[q & 1][r]), off = __builtin_fmaf((float)zp[q & 1][r], z_mul, z_add);   // -(16 + z)
+            const float scale = Elem<Tag>::to_f32((uint16_t)sc[q & 1][r]), off = ZP ? -16.f - (float)zp[q & 1][r] : 0.f;
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) res[mt][r] = __builtin_fmaf(__builtin_fmaf(off, sa[mt][q], sum[mt][r]), scale, res[mt][r]);
+            for (int mt = 0; mt < MT; ++mt) res[mt][r] = __builtin_fmaf(ZP ? __builtin_fmaf(off, sa[mt][q], sum[mt][r]) : sum[mt][r], scale, res[mt][r]);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int b = 0; b < GB; ++b)
           if (b == blk) {
+            asm volatile("");                              // (jumped over, not selected)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) add4(acc[b][mt], res[mt]);
           }
         refill(1);
       }
     }
-    // ---- the wavefronts' sums into their own rings (all their loads have landed), then the sums of those. acc register r: column 4 g + r, row r16 of the tile
-    float* own = reinterpret_cast<float*>(smem + wave * W4_RING);
-    static_assert(GB * MT * 1024 <= W4_RING, "a wavefront's sums lie in its own ring");
+    // ---- the wavefronts' sums into their own rings (all their loads have landed), as many blocks at a time as there is room for, then the sums of those.
+    // acc register r: column 4 g + r, row r16 of the tile
+    float* own = reinterpret_cast<float*>(smem + wave * RING);
+    constexpr int FIT = RING / (MT * 1024) < GB ? RING / (MT * 1024) : GB;
 #pragma unroll
-    for (int b = 0; b < GB; ++b)
-      if (b < nb) {
+    for (int b0 = 0; b0 < GB; b0 += FIT) {
+      if (b0 >= nb) break;
+      if (b0 > 0) __syncthreads();
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) *reinterpret_cast<f32x4_mem*>(own + (b * MT + mt) * 256 + r16 * 16 + 4 * g) = acc[b][mt];
-      }
-    __syncthreads();
-    for (int e = tid; e < nb * MT * 256; e += W4_NT) {
-      const int t = e >> 8, gr = t % MT * 16 + ((e >> 4) & 15), gc = c0 + (base + t / MT) * 16 + (e & 15);
-      if (gr < M && gc < c1) {
-        float sum = 0.f;
+      for (int b = b0; b < b0 + FIT && b < GB; ++b)
+        if (b < nb) {
 #pragma unroll
-        for (int w = 0; w < W4_NW; ++w) sum += reinterpret_cast<const float*>(smem)[w * (W4_RING / 4) + e];
-        if (split) store_shared(a.part + ((int64_t)part_id * a.M + m0 + gr) * N + gc, sum);
-        else a.C[(int64_t)(m0 + gr) * a.ldc + gc] = Elem<Tag>::from_f32(sum);
+          for (int mt = 0; mt < MT; ++mt) *reinterpret_cast<f32x4_mem*>(own + ((b - b0) * MT + mt) * 256 + r16 * 16 + 4 * g) = acc[b][mt];
+        }
+      __syncthreads();
+      const int here = nb - b0 < FIT ? nb - b0 : FIT;
+      for (int e = tid; e < here * MT * 256; e += NT) {
+        const int t = e >> 8, gr = t % MT * 16 + ((e >> 4) & 15), gc = c0 + (base + b0 + t / MT) * 16 + (e & 15);
+        if (gr < M && gc < c1) {
+          float sum = 0.f;
+#pragma unroll
+          for (int w = 0; w < NW; ++w) sum += reinterpret_cast<const float*>(smem)[w * (RING / 4) + e];
+          if (split) store_shared(a.part + ((int64_t)part_id * a.M + m0 + gr) * N + gc, sum);
+          else a.C[(int64_t)(m0 + gr) * a.ldc + gc] = Elem<Tag>::from_f32(sum);
+        }
       }
     }
     if (base + GB < nblk) __syncthreads();
@@ -334,12 +360,12 @@ __global__ __launch_bounds__(W4_NT, 2) void gemm_4bit_kernel(W4 a) {
   const int cols = c1 - c0, parts = (int)gridDim.y;
   const int64_t part_size = (int64_t)a.M * N;
   constexpr int EB = 4;
-  for (int e0 = tid; e0 < M * cols; e0 += EB * W4_NT) {
+  for (int e0 = tid; e0 < M * cols; e0 += EB * NT) {
     float v[8][EB];
     int64_t at[EB];
 #pragma unroll
     for (int i = 0; i < EB; ++i) {
-      const int e = e0 + i * W4_NT < M * cols ? e0 + i * W4_NT : e0;
+      const int e = e0 + i * NT < M * cols ? e0 + i * NT : e0;
       at[i] = (int64_t)(m0 + e / cols) * N + c0 + e % cols;
     }
 #pragma unroll
@@ -356,41 +382,44 @@ __global__ __launch_bounds__(W4_NT, 2) void gemm_4bit_kernel(W4 a) {
       }
 #pragma unroll
     for (int i = 0; i < EB; ++i)
-      if (e0 + i * W4_NT < M * cols) {
-        const int e = e0 + i * W4_NT;
+      if (e0 + i * NT < M * cols) {
+        const int e = e0 + i * NT;
         a.C[(int64_t)(m0 + e / cols) * a.ldc + c0 + e % cols] = Elem<Tag>::from_f32(v[0][i]);
       }
   }
 }
 
-template <typename Tag, int MT, int G, int KP, int GB>
+template <typename Tag, int MT, int G, int KP, int NW, bool ZP>
 int launch_w4(const W4& a, unsigned nwg, int parts, hipStream_t s) {
-  auto kern = gemm_4bit_kernel<Tag, MT, G, KP, GB>;
+  auto kern = gemm_4bit_kernel<Tag, MT, G, KP, NW, ZP>;
   static thread_local int configured_dev = -1;            // opt in to > 64 KB LDS once per device
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return MLT_ERR_DEVICE;
   if (configured_dev != dev) {
-    if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, W4_NW * W4_RING) != hipSuccess) {
+    if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * W4_RING) != hipSuccess) {
       (void)hipGetLastError();
       return MLT_ERR_LAUNCH;
     }
     configured_dev = dev;
   }
-  hipLaunchKernelGGL(kern, dim3(nwg, (unsigned)parts, (unsigned)((a.M + W4_ROWS - 1) / W4_ROWS)), dim3(W4_NT), W4_NW * W4_RING, s, a);
+  hipLaunchKernelGGL(kern, dim3(nwg, (unsigned)parts, (unsigned)((a.M + W4_ROWS - 1) / W4_ROWS)), dim3(NW * 64), 8 * W4_RING, s, a);
   return hipGetLastError() == hipSuccess ? MLT_OK : MLT_ERR_LAUNCH;
 }
 
-template <typename Tag, int G>
+// Up to 32 rows eight wavefronts; more leave no registers for two on a SIMD. 512 k a piece where A's tile and its groups' sums fit the registers.
+template <typename Tag, int G, bool ZP>
 int run_w4_rows(const W4& a, unsigned nwg, int parts, hipStream_t s) {
   const int rows = a.M < W4_ROWS ? a.M : W4_ROWS;
-  if (rows <= 16) return launch_w4<Tag, 1, G, G == 32 ? 256 : 512, 8>(a, nwg, parts, s);   // (there are no registers for 16 groups)
-  if (rows <= 32) return launch_w4<Tag, 2, G, 256, 8>(a, nwg, parts, s);
-  return launch_w4<Tag, 4, G, 256, 4>(a, nwg, parts, s);
+  if (rows <= 16) return launch_w4<Tag, 1, G, G == 32 ? 256 : 512, 8, ZP>(a, nwg, parts, s);
+  if (rows <= 32) return launch_w4<Tag, 2, G, 256, 8, ZP>(a, nwg, parts, s);
+  return launch_w4<Tag, 4, G, 256, 4, ZP>(a, nwg, parts, s);
 }
+int64_t piece_of(int64_t rows, int64_t group) { return rows <= 16 && group > 32 ? 512 : 256; }
+int waves_of(int64_t rows) { return rows <= 32 ? 8 : 4; }
 
-template <typename Tag>
+template <typename Tag, bool ZP>
 int run_w4_t(const W4& a, int group, unsigned nwg, int parts, hipStream_t s) {
-  return group == 32 ? run_w4_rows<Tag, 32>(a, nwg, parts, s) : group == 64 ? run_w4_rows<Tag, 64>(a, nwg, parts, s) : run_w4_rows<Tag, 128>(a, nwg, parts, s);
+  return group == 32 ? run_w4_rows<Tag, 32, ZP>(a, nwg, parts, s) : group == 64 ? run_w4_rows<Tag, 64, ZP>(a, nwg, parts, s) : run_w4_rows<Tag, 128, ZP>(a, nwg, parts, s);
 }
 
 __global__ __launch_bounds__(256) void zero_rows_kernel(uint16_t* C, int64_t ldc, int N) {
@@ -414,8 +443,8 @@ int run_gemm_4bit(const Gemm4bitArgs& g, hipStream_t s, char* name, size_t size)
   const int64_t nz = (g.M + W4_ROWS - 1) / W4_ROWS, rows = g.M < W4_ROWS ? g.M : W4_ROWS;
   // parts of K until a workgroup reads no more of A than of W (2 rows K / parts against columns K / 2 / parts), as long as each wavefront keeps a piece
   int parts = 1;
-  const int64_t kp = rows <= 16 && g.group > 32 ? 512 : 256, pieces = (g.K + kp - 1) / kp;
-  while (parts < 8 && rows * 4 * ncu > g.N * parts * 2 && pieces >= 2 * parts * W4_NW) parts *= 2;
+  const int64_t kp = piece_of(rows, g.group), pieces = (g.K + kp - 1) / kp;
+  while (parts < 8 && rows * 4 * ncu > g.N * parts * 2 && pieces >= 2 * parts * waves_of(rows)) parts *= 2;
   while (parts > 1 && (parts * g.M * g.N * 4 > (int64_t)32 << 20 || ncu / parts * nz > kScratchCounters)) parts /= 2;
   float* part = nullptr;
   if (parts > 1) {
@@ -424,11 +453,12 @@ int run_gemm_4bit(const Gemm4bitArgs& g, hipStream_t s, char* name, size_t size)
   }
   int64_t nwg = ncu / parts;
   if (nwg > (g.N + 3) / 4) nwg = (g.N + 3) / 4;
-  if (nz > 65535 || !launch_fits(nwg * parts * nz, W4_NT)) return MLT_ERR_UNSUPPORTED;
+  if (nz > 65535 || !launch_fits(nwg * parts * nz, 512)) return MLT_ERR_UNSUPPORTED;
   W4 a{(int)g.M, (int)g.N, (int)g.K, (int)(g.N / nwg), (int)(g.N % nwg), (int)g.lda, (int)g.ldw, g.A, g.W, g.S, g.Z, g.lds, g.ldz, g.C, g.ldc, part,
        part ? scratch_counters(part) : nullptr};
   snprintf(name, size, "gemm_4bit_g%d_m%d_parts%d", (int)g.group, rows <= 16 ? 16 : rows <= 32 ? 32 : 64, parts);
-  return g.dtype == MLT_BF16 ? run_w4_t<bf16_tag>(a, (int)g.group, (unsigned)nwg, parts, s) : run_w4_t<f16_tag>(a, (int)g.group, (unsigned)nwg, parts, s);
+  if (g.dtype == MLT_BF16) return g.Z ? run_w4_t<bf16_tag, true>(a, (int)g.group, (unsigned)nwg, parts, s) : run_w4_t<bf16_tag, false>(a, (int)g.group, (unsigned)nwg, parts, s);
+  return g.Z ? run_w4_t<f16_tag, true>(a, (int)g.group, (unsigned)nwg, parts, s) : run_w4_t<f16_tag, false>(a, (int)g.group, (unsigned)nwg, parts, s);
 }
 
 }  // namespace mlt
