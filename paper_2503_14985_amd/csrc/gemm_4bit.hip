@@ -15,68 +15,36 @@
 // More than 64 rows are tiles of 64, which read the weights once each.
 #include <stdio.h>
 
-#include "fp8.h"
+#include "gemm_4bit.h"
 #include "mlt_internal.h"
 
 namespace mlt {
 
 namespace {
 
-constexpr int W4_RING = 19 * 1024 + 512;   // LDS ring of a wavefront of eight: 156 KB in all
+constexpr int W4_NW = 8;
+constexpr int W4_RING = 19 * 1024 + 512;   // LDS ring of a wavefront: 156 KB in all
+constexpr int W4_ROWS = 32;                // rows up to which a wavefront keeps A's piece
 constexpr int W4_GB = 8;                   // blocks of 16 columns whose sums are kept at once
-constexpr int W4_ROWS = 64;                // rows of C of a workgroup
 
-// a 16-bit (8-bit) number for each lane (uniform base + per-lane byte offset), as a dword to lds_addr + 4 * lane
-__device__ __forceinline__ void load_lds_u16(const void* base, uint32_t voff, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %2" : : "s"(lds_addr), "v"(voff), "s"(base) : "memory", "m0");
-}
-__device__ __forceinline__ void load_lds_u8(const void* base, uint32_t voff, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2" : : "s"(lds_addr), "v"(voff), "s"(base) : "memory", "m0");
-}
-
-// 16 + q of nibbles i and i + 4. The two constants are given in registers: and-or takes no two literals.
-template <typename Tag> struct Nibbles {
-  static constexpr bool BF = __is_same(Tag, bf16_tag);
-  static constexpr uint32_t MASK = BF ? 0x00780078u : 0x03c003c0u, SIXTEEN = BF ? 0x41804180u : 0x4c004c00u;
-  static __device__ __forceinline__ uint32_t get(uint32_t w, int i, uint32_t mask, uint32_t sixteen) {
-    const int right = 4 * i - (BF ? 3 : 6);
-    return ((right < 0 ? w << -right : w >> right) & mask) | sixteen;
-  }
-};
-
-struct W4 {
-  int M, N, K, share, rest, lda, ldw;
-  const uint16_t* A;
-  const uint8_t* W;
-  const uint16_t* S;
-  const uint8_t* Z;
-  int64_t lds, ldz;                            // (below 2^26)
-  uint16_t* C;
-  int64_t ldc;
-  float* part;
-  uint32_t* counter;
-};
-
-// MT: 16-row tiles of A; G: group; KP: k of a piece; NW: wavefronts; ZP: with zero points
-template <typename Tag, int MT, int G, int KP, int NW, bool ZP>
-__global__ __launch_bounds__(NW * 64, NW / 4) void gemm_4bit_kernel(W4 a) {
+// MT: 16-row tiles of A; G: group; KP: k of a piece; ZP: with zero points
+template <typename Tag, int MT, int G, int KP, bool ZP>
+__global__ __launch_bounds__(W4_NW * 64, 2) void gemm_4bit_kernel(W4 a) {
   typedef typename Elem<Tag>::vec8 V8;
-  constexpr int GB = W4_GB, NT = NW * 64;
-  constexpr int RING = 8 * W4_RING / NW;                   // LDS ring of a wavefront
+  constexpr int GB = W4_GB, NW = W4_NW, NT = NW * 64;
   constexpr int NS = KP / 32, NG = KP / G, SPG = G / 32;   // steps and groups of a piece, steps of a group
   constexpr int AROW = KP * 2, WROW = KP / 2;              // bytes of a row
   constexpr int ARI = 1024 / AROW, WRI = 1024 / WROW;      // rows of a load
   constexpr int BODY = 4 * AROW, NL = BODY / 1024;         // a slot holds 4 rows of A or 16 of W: loads of it
   constexpr int NSL = (NG * 16 + 63) / 64;                 // loads of a block's scales, of its zero points
-  constexpr int SIDE = NSL * 256, SLOT = BODY + SIDE * (ZP ? 2 : 1), SLOTS = RING / SLOT, W_LOADS = NL + NSL * (ZP ? 2 : 1);
+  constexpr int SIDE = NSL * 256, SLOT = BODY + SIDE * (ZP ? 2 : 1), SLOTS = W4_RING / SLOT, W_LOADS = NL + NSL * (ZP ? 2 : 1);
   constexpr bool WHOLE = SLOTS >= 5;                       // room for a tile of A and more
   static_assert(BODY == 16 * WROW, "one size for both");
   static_assert(WHOLE || MT == 1, "a tile of A slot by slot: its zeros and sums are those of the last one");
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, g = lane >> 4;
-  const int m0 = (int)blockIdx.z * W4_ROWS, M = a.M - m0 < W4_ROWS ? a.M - m0 : W4_ROWS, N = a.N, K = a.K;
-  const uint16_t* const A = a.A + (int64_t)m0 * a.lda;
+  const int M = a.M, N = a.N, K = a.K;
   const int bid = (int)blockIdx.x, part_id = (int)blockIdx.y;
   const bool split = gridDim.y > 1;
   const int c0 = bid * a.share + (bid < a.rest ? bid : a.rest), c1 = c0 + a.share + (bid < a.rest ? 1 : 0), nblk = (c1 - c0 + 15) / 16;
@@ -92,7 +60,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void gemm_4bit_kernel(W4 a) {
   // not: that would be the same few memory channels.
   const int start = mine > 0 ? first + (wave + bid) % mine * NW : first;
   const int last_group = (K - 1) / G;
-  const uint32_t ring = (uint32_t)(uintptr_t)(lptr_t)smem + (uint32_t)wave * RING, ring_end = ring + SLOTS * SLOT;
+  const uint32_t ring = (uint32_t)(uintptr_t)(lptr_t)smem + (uint32_t)wave * W4_RING, ring_end = ring + SLOTS * SLOT;
   const int SA = (M + 3) / 4;                              // slots of A
 
   // A: row 4 i + n of slot i is row n of it, chunk c (8 k) at position c ^ row (low four bits); W: chunk c (32 k) of row n at position c ^ f(n)
@@ -115,7 +83,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void gemm_4bit_kernel(W4 a) {
   const uint32_t a_row = (uint32_t)a_in * (uint32_t)a.lda * 2u, a_chunk = (uint32_t)(((lane % ACH) ^ a_in) * 16);
   // this lane's places in a slot of A (its chunk 4 s + g by XOR, slots begin on 256 bytes) and of W (its word of chunk s)
   const uint32_t a_lane = (uint32_t)((r16 & 3) * AROW + ((g ^ r16) << 4)), w_lane = (uint32_t)(r16 * WROW + (fw(r16) << 4) + 4 * g);
-  static_assert(RING % 256 == 0 && SLOT % 256 == 0 && W4_RING % 256 == 0, "see a_lane");
+  static_assert(W4_RING % 256 == 0 && SLOT % 256 == 0, "see a_lane");
   uint32_t mask = Nibbles<Tag>::MASK, sixteen = Nibbles<Tag>::SIXTEEN;
   asm volatile("" : "+v"(mask), "+v"(sixteen));
 
@@ -135,7 +103,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void gemm_4bit_kernel(W4 a) {
     const uint8_t *f_w = nullptr, *f_z = nullptr;
     auto piece_begins = [&]() __attribute__((always_inline)) {
       const int k0 = f_p * KP;
-      f_a = A + k0;
+      f_a = a.A + k0;
       f_rows = M;
       f_w = a.W + (int64_t)(c0 + base * 16) * a.ldw + k0 / 2;
       f_sc = a.S + k0 / G * a.lds + c0 + base * 16;
@@ -326,8 +294,8 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void gemm_4bit_kernel(W4 a) {
     }
     // ---- the wavefronts' sums into their own rings (all their loads have landed), as many blocks at a time as there is room for, then the sums of those.
     // acc register r: column 4 g + r, row r16 of the tile
-    float* own = reinterpret_cast<float*>(smem + wave * RING);
-    constexpr int FIT = RING / (MT * 1024) < GB ? RING / (MT * 1024) : GB;
+    float* own = reinterpret_cast<float*>(smem + wave * W4_RING);
+    constexpr int FIT = W4_RING / (MT * 1024) < GB ? W4_RING / (MT * 1024) : GB;
 #pragma unroll
     for (int b0 = 0; b0 < GB; b0 += FIT) {
       if (b0 >= nb) break;
@@ -345,9 +313,9 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void gemm_4bit_kernel(W4 a) {
         if (gr < M && gc < c1) {
           float sum = 0.f;
 #pragma unroll
-          for (int w = 0; w < NW; ++w) sum += reinterpret_cast<const float*>(smem)[w * (RING / 4) + e];
-          if (split) store_shared(a.part + ((int64_t)part_id * a.M + m0 + gr) * N + gc, sum);
-          else a.C[(int64_t)(m0 + gr) * a.ldc + gc] = Elem<Tag>::from_f32(sum);
+          for (int w = 0; w < NW; ++w) sum += reinterpret_cast<const float*>(smem)[w * (W4_RING / 4) + e];
+          if (split) store_shared(a.part + ((int64_t)part_id * M + gr) * N + gc, sum);
+          else a.C[(int64_t)gr * a.ldc + gc] = Elem<Tag>::from_f32(sum);
         }
       }
     }
@@ -355,67 +323,33 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void gemm_4bit_kernel(W4 a) {
   }
   if (!split) return;
 
-  // the last part of these columns to get here adds them all (4 elements of a thread at a time, all their parts requested before the first is used)
-  if (!last_to_arrive(a.counter + bid * (int)gridDim.z + (int)blockIdx.z, gridDim.y, reinterpret_cast<uint32_t*>(smem))) return;
-  const int cols = c1 - c0, parts = (int)gridDim.y;
-  const int64_t part_size = (int64_t)a.M * N;
-  constexpr int EB = 4;
-  for (int e0 = tid; e0 < M * cols; e0 += EB * NT) {
-    float v[8][EB];
-    int64_t at[EB];
-#pragma unroll
-    for (int i = 0; i < EB; ++i) {
-      const int e = e0 + i * NT < M * cols ? e0 + i * NT : e0;
-      at[i] = (int64_t)(m0 + e / cols) * N + c0 + e % cols;
-    }
-#pragma unroll
-    for (int p = 0; p < 8; ++p)
-      if (p < parts) {
-#pragma unroll
-        for (int i = 0; i < EB; ++i) v[p][i] = load_shared(a.part + p * part_size + at[i]);
-      }
-#pragma unroll
-    for (int p = 1; p < 8; ++p)
-      if (p < parts) {
-#pragma unroll
-        for (int i = 0; i < EB; ++i) v[0][i] += v[p][i];
-      }
-#pragma unroll
-    for (int i = 0; i < EB; ++i)
-      if (e0 + i * NT < M * cols) {
-        const int e = e0 + i * NT;
-        a.C[(int64_t)(m0 + e / cols) * a.ldc + c0 + e % cols] = Elem<Tag>::from_f32(v[0][i]);
-      }
-  }
+  if (!last_to_arrive(a.counter + bid, gridDim.y, reinterpret_cast<uint32_t*>(smem))) return;
+  w4_add_parts<Tag, NT>(a, (int)gridDim.y, 0, M, c0, c1);
 }
 
-template <typename Tag, int MT, int G, int KP, int NW, bool ZP>
+template <typename Tag, int MT, int G, int KP, bool ZP>
 int launch_w4(const W4& a, unsigned nwg, int parts, hipStream_t s) {
-  auto kern = gemm_4bit_kernel<Tag, MT, G, KP, NW, ZP>;
+  auto kern = gemm_4bit_kernel<Tag, MT, G, KP, ZP>;
   static thread_local int configured_dev = -1;            // opt in to > 64 KB LDS once per device
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return MLT_ERR_DEVICE;
   if (configured_dev != dev) {
-    if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * W4_RING) != hipSuccess) {
+    if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, W4_NW * W4_RING) != hipSuccess) {
       (void)hipGetLastError();
       return MLT_ERR_LAUNCH;
     }
     configured_dev = dev;
   }
-  hipLaunchKernelGGL(kern, dim3(nwg, (unsigned)parts, (unsigned)((a.M + W4_ROWS - 1) / W4_ROWS)), dim3(NW * 64), 8 * W4_RING, s, a);
+  hipLaunchKernelGGL(kern, dim3(nwg, (unsigned)parts), dim3(W4_NW * 64), W4_NW * W4_RING, s, a);
   return hipGetLastError() == hipSuccess ? MLT_OK : MLT_ERR_LAUNCH;
 }
 
-// Up to 32 rows eight wavefronts; more leave no registers for two on a SIMD. 512 k a piece where A's tile and its groups' sums fit the registers.
+// 512 k a piece where A's tile and its groups' sums fit the registers.
 template <typename Tag, int G, bool ZP>
 int run_w4_rows(const W4& a, unsigned nwg, int parts, hipStream_t s) {
-  const int rows = a.M < W4_ROWS ? a.M : W4_ROWS;
-  if (rows <= 16) return launch_w4<Tag, 1, G, G == 32 ? 256 : 512, 8, ZP>(a, nwg, parts, s);
-  if (rows <= 32) return launch_w4<Tag, 2, G, 256, 8, ZP>(a, nwg, parts, s);
-  return launch_w4<Tag, 4, G, 256, 4, ZP>(a, nwg, parts, s);
+  if (a.M <= 16) return launch_w4<Tag, 1, G, G == 32 ? 256 : 512, ZP>(a, nwg, parts, s);
+  return launch_w4<Tag, 2, G, 256, ZP>(a, nwg, parts, s);
 }
-int64_t piece_of(int64_t rows, int64_t group) { return rows <= 16 && group > 32 ? 512 : 256; }
-int waves_of(int64_t rows) { return rows <= 32 ? 8 : 4; }
 
 template <typename Tag, bool ZP>
 int run_w4_t(const W4& a, int group, unsigned nwg, int parts, hipStream_t s) {
@@ -440,25 +374,39 @@ int run_gemm_4bit(const Gemm4bitArgs& g, hipStream_t s, char* name, size_t size)
   }
   DeviceInfo di;
   const int64_t ncu = device_info(di) && di.ncu > 0 ? di.ncu : 256;
-  const int64_t nz = (g.M + W4_ROWS - 1) / W4_ROWS, rows = g.M < W4_ROWS ? g.M : W4_ROWS;
-  // parts of K until a workgroup reads no more of A than of W (2 rows K / parts against columns K / 2 / parts), as long as each wavefront keeps a piece
-  int parts = 1;
-  const int64_t kp = piece_of(rows, g.group), pieces = (g.K + kp - 1) / kp;
-  while (parts < 8 && rows * 4 * ncu > g.N * parts * 2 && pieces >= 2 * parts * waves_of(rows)) parts *= 2;
-  while (parts > 1 && (parts * g.M * g.N * 4 > (int64_t)32 << 20 || ncu / parts * nz > kScratchCounters)) parts /= 2;
-  float* part = nullptr;
-  if (parts > 1) {
-    part = cached_scratch(parts * g.M * g.N * 4, s);
-    if (!part) parts = 1;
+  W4 a{(int)g.M, (int)g.N, (int)g.K, 0, 0, (int)g.lda, (int)g.ldw, g.A, g.W, g.S, g.Z, g.lds, g.ldz, g.C, g.ldc, nullptr, nullptr};
+  const bool tile = g.M > W4_ROWS;
+  const int64_t rows = g.M <= 16 ? 16 : g.M <= 32 ? 32 : g.M <= 64 ? 64 : 128, nz = (g.M + rows - 1) / rows, blocks = (g.N + 15) / 16;
+  int64_t nwg = (blocks + 7) / 8, parts = 1;
+  if (tile) {
+    const int64_t chunks = (g.K + 127) / 128;
+    int64_t best = 0;
+    for (int64_t p = 1; p <= 16 && (p == 1 || p * 2 <= chunks); ++p) {
+      const int64_t cost = (nwg * nz * p + ncu - 1) / ncu * ((chunks + p - 1) / p + 4) + (p > 1 ? 2 + p / 2 : 0);
+      if (p == 1 || cost < best) best = cost, parts = p;
+    }
+  } else {
+    // parts of K until a workgroup reads no more of A than of W (2 rows K / parts against columns K / 2 / parts), as long as each wavefront keeps a piece
+    const int64_t kp = rows <= 16 && g.group > 32 ? 512 : 256, pieces = (g.K + kp - 1) / kp;
+    while (parts < 8 && rows * 4 * ncu > g.N * parts * 2 && pieces >= 2 * parts * W4_NW) parts *= 2;
   }
-  int64_t nwg = ncu / parts;
-  if (nwg > (g.N + 3) / 4) nwg = (g.N + 3) / 4;
-  if (nz > 65535 || !launch_fits(nwg * parts * nz, 512)) return MLT_ERR_UNSUPPORTED;
-  W4 a{(int)g.M, (int)g.N, (int)g.K, (int)(g.N / nwg), (int)(g.N % nwg), (int)g.lda, (int)g.ldw, g.A, g.W, g.S, g.Z, g.lds, g.ldz, g.C, g.ldc, part,
-       part ? scratch_counters(part) : nullptr};
-  snprintf(name, size, "gemm_4bit_g%d_m%d_parts%d", (int)g.group, rows <= 16 ? 16 : rows <= 32 ? 32 : 64, parts);
-  if (g.dtype == MLT_BF16) return g.Z ? run_w4_t<bf16_tag, true>(a, (int)g.group, (unsigned)nwg, parts, s) : run_w4_t<bf16_tag, false>(a, (int)g.group, (unsigned)nwg, parts, s);
-  return g.Z ? run_w4_t<f16_tag, true>(a, (int)g.group, (unsigned)nwg, parts, s) : run_w4_t<f16_tag, false>(a, (int)g.group, (unsigned)nwg, parts, s);
+  while (parts > 1 && (parts * g.M * g.N * 4 > (int64_t)32 << 20 || (tile ? nwg * nz : ncu / parts) > kScratchCounters)) parts /= 2;
+  if (parts > 1) {
+    a.part = cached_scratch(parts * g.M * g.N * 4, s);
+    if (a.part) a.counter = scratch_counters(a.part);
+    else parts = 1;
+  }
+  if (!tile) {
+    nwg = ncu / parts;
+    if (nwg > (g.N + 3) / 4) nwg = (g.N + 3) / 4;
+  }
+  a.share = (int)((tile ? blocks : g.N) / nwg);
+  a.rest = (int)((tile ? blocks : g.N) % nwg);
+  if (nz > 65535 || !launch_fits(nwg * parts * nz, W4_NW * 64)) return MLT_ERR_UNSUPPORTED;
+  snprintf(name, size, "gemm_4bit_g%d_m%d_parts%d", (int)g.group, (int)rows, (int)parts);
+  if (tile) return run_w4_tile(a, g.dtype, (int)g.group, (int)rows, (unsigned)nwg, (int)parts, s);
+  if (g.dtype == MLT_BF16) return g.Z ? run_w4_t<bf16_tag, true>(a, (int)g.group, (unsigned)nwg, (int)parts, s) : run_w4_t<bf16_tag, false>(a, (int)g.group, (unsigned)nwg, (int)parts, s);
+  return g.Z ? run_w4_t<f16_tag, true>(a, (int)g.group, (unsigned)nwg, (int)parts, s) : run_w4_t<f16_tag, false>(a, (int)g.group, (unsigned)nwg, (int)parts, s);
 }
 
 }  // namespace mlt
