@@ -74,7 +74,8 @@ template <typename Tag, int NT> __device__ __forceinline__ void w4_add_parts(con
   }
 }
 
-// gemm_4bit_tile.hip
-int run_w4_tile(const W4& a, int dtype, int group, int rows, unsigned nwg, int parts, hipStream_t s);
+// gemm_4bit_tile.hip: nwg workgroups of up to 8 or 16 blocks of 16 columns for every 64 rows and each part of K
+constexpr int W4T_ROWS = 64;
+int run_w4_tile(const W4& a, int dtype, int group, int blocks, unsigned nwg, int parts, hipStream_t s);
 
 }  // namespace mlt

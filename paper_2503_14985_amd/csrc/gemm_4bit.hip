@@ -376,9 +376,11 @@ int run_gemm_4bit(const Gemm4bitArgs& g, hipStream_t s, char* name, size_t size)
   const int64_t ncu = device_info(di) && di.ncu > 0 ? di.ncu : 256;
   W4 a{(int)g.M, (int)g.N, (int)g.K, 0, 0, (int)g.lda, (int)g.ldw, g.A, g.W, g.S, g.Z, g.lds, g.ldz, g.C, g.ldc, nullptr, nullptr};
   const bool tile = g.M > W4_ROWS;
-  const int64_t rows = g.M <= 16 ? 16 : g.M <= 32 ? 32 : g.M <= 64 ? 64 : 128, nz = (g.M + rows - 1) / rows, blocks = (g.N + 15) / 16;
-  int64_t nwg = (blocks + 7) / 8, parts = 1;
+  const int64_t rows = g.M <= 16 ? 16 : g.M <= 32 ? 32 : W4T_ROWS, nz = (g.M + rows - 1) / rows, blocks = (g.N + 15) / 16;
+  const int64_t wide = (blocks + 15) / 16 * nz * 4 >= ncu ? 16 : 8;   // blocks of a tile (gemm_4bit_tile.hip has the figures)
+  int64_t nwg = (blocks + wide - 1) / wide, parts = 1;
   if (tile) {
+    // parts of K: rounds of workgroups, each of its chunks and some 4 chunks' time to begin and end, and the kernel that adds them
     const int64_t chunks = (g.K + 127) / 128;
     int64_t best = 0;
     for (int64_t p = 1; p <= 16 && (p == 1 || p * 2 <= chunks); ++p) {
@@ -390,7 +392,7 @@ int run_gemm_4bit(const Gemm4bitArgs& g, hipStream_t s, char* name, size_t size)
     const int64_t kp = rows <= 16 && g.group > 32 ? 512 : 256, pieces = (g.K + kp - 1) / kp;
     while (parts < 8 && rows * 4 * ncu > g.N * parts * 2 && pieces >= 2 * parts * W4_NW) parts *= 2;
   }
-  while (parts > 1 && (parts * g.M * g.N * 4 > (int64_t)32 << 20 || (tile ? nwg * nz : ncu / parts) > kScratchCounters)) parts /= 2;
+  while (parts > 1 && (parts * g.M * g.N * 4 > (int64_t)32 << 20 || (!tile && ncu / parts > kScratchCounters))) parts /= 2;
   if (parts > 1) {
     a.part = cached_scratch(parts * g.M * g.N * 4, s);
     if (a.part) a.counter = scratch_counters(a.part);
@@ -402,9 +404,9 @@ int run_gemm_4bit(const Gemm4bitArgs& g, hipStream_t s, char* name, size_t size)
   }
   a.share = (int)((tile ? blocks : g.N) / nwg);
   a.rest = (int)((tile ? blocks : g.N) % nwg);
-  if (nz > 65535 || !launch_fits(nwg * parts * nz, W4_NW * 64)) return MLT_ERR_UNSUPPORTED;
+  if (nz > 65535 || !launch_fits(nwg * parts * nz, 512)) return MLT_ERR_UNSUPPORTED;
   snprintf(name, size, "gemm_4bit_g%d_m%d_parts%d", (int)g.group, (int)rows, (int)parts);
-  if (tile) return run_w4_tile(a, g.dtype, (int)g.group, (int)rows, (unsigned)nwg, (int)parts, s);
+  if (tile) return run_w4_tile(a, g.dtype, (int)g.group, (int)wide, (unsigned)nwg, (int)parts, s);
   if (g.dtype == MLT_BF16) return g.Z ? run_w4_t<bf16_tag, true>(a, (int)g.group, (unsigned)nwg, (int)parts, s) : run_w4_t<bf16_tag, false>(a, (int)g.group, (unsigned)nwg, (int)parts, s);
   return g.Z ? run_w4_t<f16_tag, true>(a, (int)g.group, (unsigned)nwg, (int)parts, s) : run_w4_t<f16_tag, false>(a, (int)g.group, (unsigned)nwg, (int)parts, s);
 }
