@@ -327,7 +327,8 @@ int mlt_paged_attn_prompt(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D
  *   work           device, 16-byte aligned, work_bytes long: fp32 partial results, needed only while the call runs; or NULL: the library's scratch of the stream. With less than
  *                  mlt_paged_attn_decode_prefix_work says, or NULL on a stream that records into a graph, the prefix is read again for
  *                  every sequence. Two captured graphs that may run at the same time need a work of their own each.
- * Weights keep about 16 bits or more whatever `dtype`. The limits of what is read, clamping and requirements are those of mlt_paged_attn_decode_fp8;
+ * Weights of own keys keep about 16 bits or more whatever `dtype`, as do those of the prefix where it is read for up to 32 queries of a key head (B * Hq / H); for more,
+ * they are rounded to `dtype`, as in mlt_mha_fwd. An infinity or NaN in a value makes the outputs of the sequences that see it non-finite. The limits of what is read, clamping and requirements are those of mlt_paged_attn_decode_fp8;
  * prefix_len must lie in 0 .. max_blocks * block_size (MLT_ERR_INVALID_ARG).
  */
 int mlt_paged_attn_decode_prefix(int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks, int64_t num_blocks,
@@ -346,9 +347,10 @@ int64_t mlt_paged_attn_decode_prefix_work(int64_t B, int64_t Hq, int64_t H, int6
  *   Z       device, uint8 [ceil(K / group)][N], row stride ldz >= N: z, 0 .. 15; or NULL: z = 8 (ldz unused)
  *   C       device, M x N row-major of `dtype`, row stride ldc >= N; written, never read
  * group is 32, 64 or 128; the last one of a row may be shorter. Products and the sum over a group are fp32, as is the sum over the groups, each times its scale; C is
- * rounded once. An infinity in a row of A may give NaN. The order of the sums goes by the sizes; equal calls give equal bits. K a multiple of 32, lda a multiple of 8,
- * ldw of 16 (MLT_ERR_UNSUPPORTED); A and Wq 16-byte, S and C 2-byte aligned. Any M is taken; the kernel is made for up to 64 rows (the weights are read again for
- * every 64). M == 0 or N == 0 is a no-op, K == 0 stores zeros.
+ * rounded once. An infinity in a row of A, or a scale that is infinite, may give NaN in its row, or column. The order of the sums goes by the sizes (and by whether the
+ * library's scratch is to be had: a first call that a stream records into a graph); equal calls give equal bits. K a multiple of 32, lda a multiple of 8,
+ * ldw of 16, lda below 2^23, ldw below 2^25, lds and ldz below 2^26 (MLT_ERR_UNSUPPORTED); A and Wq 16-byte, S and C 2-byte aligned. Any M is taken; the kernels are made
+ * for up to 64 rows (the weights are read again for every 64). M == 0 or N == 0 is a no-op, K == 0 stores zeros.
  */
 int mlt_gemm_w4(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const void* Wq, int64_t ldw, int64_t group, const void* S, int64_t lds,
                 const uint8_t* Z, int64_t ldz, void* C, int64_t ldc, int dtype, void* stream);

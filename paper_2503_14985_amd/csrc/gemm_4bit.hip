@@ -12,7 +12,7 @@
 //   * Scales are applied to the fp32 sums of groups. They come in the same stream, a 16-bit number (zero points: 8-bit) for each lane of a load.
 //   * With few columns a CU fetches more of A than of W; K is then split over 2, 4 or 8 workgroups (split), whose fp32 partial results the one that comes last at a counter adds in the
 //     order of the parts.
-// More than 64 rows are tiles of 64, which read the weights once each.
+// More than 32 rows: gemm_4bit_tile.hip.
 #include <stdio.h>
 
 #include "gemm_4bit.h"

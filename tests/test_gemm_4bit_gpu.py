@@ -85,3 +85,24 @@ def test_empty(binding):
         C = binding.mlt_gemm_w4(torch.zeros((M, K), dtype=BF, device="cuda"), torch.zeros((N, K // 2), dtype=torch.uint8, device="cuda"),
                                 torch.zeros((-(-K // 128), N), dtype=BF, device="cuda"))
         assert C.shape == (M, N) and bool((C == 0).all())
+
+
+@pytest.mark.parametrize("M", [1, 20, 40])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_values_that_are_not_finite(binding, M, group):
+    """An infinite scale and rows with an infinity or NaN reach what they belong to and nothing else; the last part of K is shorter than what is read at a time."""
+    N, K = 100, 544
+    A, Wq, S, Z, q = w4_inputs(M, M, N, K, group, True, BF)
+    clean = binding.mlt_gemm_w4(A, Wq, S, Z, group=group)
+    S[-1, 7] = float("inf")
+    C = binding.mlt_gemm_w4(A, Wq, S, Z, group=group)
+    assert not bool(torch.isfinite(C[:, 7]).any())
+    other = torch.arange(N, device="cuda") != 7
+    assert torch.equal(C[:, other], clean[:, other])
+    S[-1, 7] = 1
+    A[M // 2, K - 1] = float("nan")
+    A[0, 0] = float("inf")
+    C = binding.mlt_gemm_w4(A, Wq, S, Z, group=group)
+    rows = torch.arange(M, device="cuda")
+    bad = (rows == M // 2) | (rows == 0)
+    assert not bool(torch.isfinite(C[bad]).any()) and torch.equal(C[~bad][:, other], clean[~bad][:, other])
