@@ -283,6 +283,11 @@ struct PromptKernel {
   int negate;
 };
 
+constexpr int kPromptPart = 512;                     // keys that a part of an item has at least
+
+// prompt_split.hip: `parts` workgroups to an item; scratch: T * Hq * parts * (D + 2) numbers
+int run_prompt_split(const PromptKernel& p, int dtype, int D, int64_t grid, int parts, float* scratch, hipStream_t s);
+
 // exponent all ones: a number that is not finite
 template <typename Tag>
 __device__ __forceinline__ bool wild(uint32_t pair, int half) {
@@ -339,7 +344,7 @@ __device__ __forceinline__ uint32_t prompt_redo(const PromptKernel& p, const Pro
 //
 // The largest weight of a row lies between 1 and 2^8 (the reference moves when the maximum has grown by 8): fp16 weights lose nothing but what is below 2^-25 of it. Weights are
 // rounded to 16 bits for the second product, and it is the rounded ones that are summed: what the rounding does to a row's weights as a whole cancels.
-// What a workgroup does of an item when its keys are split over several (not causal): tiles t0 .. t0 + tiles - 1 of them; the result goes, in fp32 and not divided by the sum, to
+// What a workgroup does of an item when its keys are split over several: tiles t0 .. t0 + tiles - 1 of them; the result goes, in fp32 and not divided by the sum, to
 // o[(row * parts + part) * D ...], its maximum (log2 domain) and sum to s[(row * parts + part) * 2 ...]; row: of Q, all heads counted.
 struct PromptPart {
   int t0, tiles, part, parts;
@@ -368,8 +373,11 @@ __device__ __forceinline__ void prompt_body(const PromptKernel& p, const PromptS
   const int my_tok = (my_r < last_r ? my_r : last_r) / G;   // (rows past the last one repeat it and are not stored)
 
   // Keys that row r sees: those before end(r) (all of them without the mask), none where that is 0 or less.
-  const int shift = m - seq.n + 1;
-  auto end_of = [&](int r) { return CAUSAL ? shift + uniform((r < last_r ? r : last_r) / G) : m; };
+  const int shift = seq.m - key0 - seq.n + 1;
+  auto end_of = [&](int r) {
+    const int end = CAUSAL ? shift + uniform((r < last_r ? r : last_r) / G) : m;
+    return SPLIT && end > m ? m : end;
+  };
   const int wg_end = end_of((qt + 1) * PA_BM - 1), w_first = end_of(q0), w_end = end_of(q0 + 31), my_end = CAUSAL ? shift + my_tok : m;
   const int my_last = my_end - 1 - 4 * h;                // ... from the first key that this lane holds of 8
   const int nblk = wg_end > 0 ? (wg_end + PA_BN - 1) / PA_BN : 0;
@@ -636,6 +644,7 @@ __device__ __forceinline__ void prompt_body(const PromptKernel& p, const PromptS
         part.s[2 * at] = mc_run;
         part.s[2 * at + 1] = l_tot;
       }
+      if (nblk == 0) return;                             // (no keys: nothing that anyone reads)
       // register quad g of tile t holds d = 32 t + 8 g + 4 h .. + 3
 #pragma unroll
       for (int t = 0; t < NDT; ++t)

@@ -202,3 +202,60 @@ def test_no_sequences_no_keys(binding):
     assert bool((O == 2).all())
     binding.mlt_mha_packed_fwd(Q, K, K, ints([0, 3]), ints([0, 0]), 0.1, causal=False, O=O)
     assert bool((O[:3] == 0).all()) and bool((O[3:] == 2).all())
+
+
+# Few rows and long keys: the keys are split over several workgroups
+BEHIND = {
+    "one": [(16, 4000)],
+    "token": [(1, 8191)],
+    "chunk": [(300, 2816)],
+    "four": [(3, 1300), (40, 2600), (0, 700), (7, 7)],
+    "empty_rows": [(20, 7), (9, 0), (70, 64), (2, 4000)],
+}
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("how", ["causal", "full", "paged"])
+@pytest.mark.parametrize("name", list(BEHIND))
+def test_split_keys(binding, name, how, D, dtype):
+    batch = BEHIND[name]
+    cu, ku, Q, K, V = make(len(name), batch, 8, 2, D, dtype, lead=2, trail=3)
+    O = torch.full_like(Q, 5.0)
+    scale = 1.0 / math.sqrt(D)
+    lens = [m for _, m in batch]
+    if how == "paged":
+        Kc, Vc, table = cache_of(9, lens, 2, D, 48, dtype)
+        for b, m in enumerate(lens):                                 # slots behind a sequence's last key: anything
+            if m % 48:
+                Kc[table[b, m // 48].long(), :, m % 48:] = math.nan
+                Vc[table[b, m // 48].long(), :, m % 48:] = math.inf
+        for _ in range(2):
+            binding.mlt_paged_attn_prompt(Q, Kc, Vc, ints(cu), ints(lens), table, scale, O=O)
+        K, V = (torch.cat([K[:2]] + [rows_of(c, table[b, :-(-m // 48)], m) for b, m in enumerate(lens)]) for c in (Kc, Vc))
+    else:
+        binding.mlt_mha_packed_fwd(Q, K, V, ints(cu), ints(ku), scale, causal=how == "causal", O=O)
+    assert "parts" in binding.mlt_last_kernel()
+    assert bool((O[:2] == 5).all()) and bool((O[cu[-1]:] == 5).all())
+    check_packed(O, Q, K, V, cu, ku, scale, how != "full", what=binding.mlt_last_kernel())
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("D", [64, 128])
+def test_split_unseen_keys_have_no_influence(binding, D, bad):
+    batch = [(40, 2040), (30, 1500)]
+    cu, ku, Q, K, V = make(5, batch, 4, 2, D, BF)
+    scale = 1.0 / math.sqrt(D)
+    for at, b in ((ku[0] + 2020, 0), (ku[0] + 2039, 0), (ku[1] + 1490, 1)):
+        for which in (K, V):
+            dirty = which.clone()
+            dirty[at] = bad
+            O = binding.mlt_mha_packed_fwd(Q, dirty if which is K else K, dirty if which is V else V, ints(cu), ints(ku), scale)
+            assert "parts" in binding.mlt_last_kernel()
+            first = cu[b] + at - ku[b] - (batch[b][1] - batch[b][0])             # the first query that sees it
+            n, m = first - cu[b], at - ku[b]
+            check_packed(O[cu[b]:first], Q[cu[b]:first], K[ku[b]:ku[b] + m], V[ku[b]:ku[b] + m], [0, n], [0, m], scale, True, what="key %d" % at)
+            o = 1 - b
+            check_packed(O[cu[o]:cu[o + 1]], Q[cu[o]:cu[o + 1]], K[ku[o]:ku[o + 1]], V[ku[o]:ku[o + 1]], [0, batch[o][0]], [0, batch[o][1]], scale, True)
+            if which is V:
+                assert not bool(torch.isfinite(O[first:cu[b + 1]]).any())
