@@ -441,7 +441,9 @@ PrefixPlan plan_prefix(const PrefixArgs& a, int64_t ncu) {
     p.pre_per = (int)(p.pre == 3 ? per : per * PX_NW);
   }
   const int64_t left = p.pre ? units : units + (a.prefix_len + 31) / 32;
-  p.waves = left <= 4 ? 2 : left <= 16 ? 4 : 8;
+  // wavefronts of an item: some 8 to 16 units each, and more of them while there are few items
+  p.waves = left <= 34 ? 2 : left <= 68 ? 4 : 8;
+  while (p.waves < 8 && items * p.waves < ncu) p.waves *= 2;
   int64_t n = 2 * ncu / items;
   if (n > left / (2 * p.waves)) n = left / (2 * p.waves);
   if (n > PX_MAX_PARTS / 2) n = PX_MAX_PARTS / 2;
