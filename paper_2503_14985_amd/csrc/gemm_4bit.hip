@@ -357,7 +357,7 @@ int run_w4_t(const W4& a, int group, unsigned nwg, int parts, hipStream_t s) {
 }
 
 __global__ __launch_bounds__(256) void zero_rows_kernel(uint16_t* C, int64_t ldc, int N) {
-  for (int n = (int)blockIdx.x * 256 + threadIdx.x; n < N; n += (int)gridDim.x * 256) C[(int64_t)blockIdx.y * ldc + n] = 0;
+  for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < N; n += (int64_t)gridDim.x * 256) C[(int64_t)blockIdx.y * ldc + n] = 0;
 }
 
 }  // namespace
@@ -365,9 +365,10 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(uint16_t* C, int64_t ldc
 int run_gemm_4bit(const Gemm4bitArgs& g, hipStream_t s, char* name, size_t size) {
   if (g.K == 0) {
     snprintf(name, size, "gemm_4bit_zero");
-    for (int64_t r = 0; r < g.M; r += 65535) {
-      const int64_t n = g.M - r < 65535 ? g.M - r : 65535;
-      hipLaunchKernelGGL(zero_rows_kernel, dim3((unsigned)((g.N + 2047) / 2048), (unsigned)n), dim3(256), 0, s, g.C + r * g.ldc, g.ldc, (int)g.N);
+    const int64_t wide = (g.N + 2047) / 2048, high = ((int64_t)1 << 23) / wide < 65535 ? ((int64_t)1 << 23) / wide : 65535;   // (a launch has 2^32 work-items at most)
+    for (int64_t r = 0; r < g.M; r += high) {
+      const int64_t n = g.M - r < high ? g.M - r : high;
+      hipLaunchKernelGGL(zero_rows_kernel, dim3((unsigned)wide, (unsigned)n), dim3(256), 0, s, g.C + r * g.ldc, g.ldc, (int)g.N);
       if (hipGetLastError() != hipSuccess) return MLT_ERR_LAUNCH;
     }
     return MLT_OK;
