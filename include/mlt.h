@@ -19,11 +19,11 @@
  *     nothing aborts. On an error nothing has been enqueued.
  *     The 8-bit operators say themselves which of their tensors are e4m3 or fp32.
  *   - Device memory of the library's own: the GEMM entry points (few tiles against a long K),
- *     mlt_paged_attn_decode and its 8-bit form (few sequences x heads) and mlt_mha_fwd (few query tiles against many
- *     keys) may spread one result over several workgroups and then keep fp32 partial results in a
+ *     mlt_paged_attn_decode and its 8-bit form (few sequences x heads), mlt_mha_fwd and the attention of packed sequences and prompts (few query tiles against many
+ *     keys) and mlt_paged_attn_decode_prefix (unless it is given `work`) may spread one result over several workgroups and then keep fp32 partial results in a
  *     scratch buffer, one per (device, stream), allocated with hipMalloc at the first call that
- *     needs it, grown by doubling from 4 MiB (32 MiB covers every split the library chooses by
- *     itself) and kept until the process ends. Calls on one stream are ordered by the stream; calls
+ *     needs it, grown by doubling from 4 MiB (64 MiB covers every split the library chooses by
+ *     itself, but for shared prefixes of very large batches) and kept until the process ends. Calls on one stream are ordered by the stream; calls
  *     on different streams use different buffers (on hipStreamPerThread: of different threads). If the allocation fails, or the stream is
  *     recording into a graph (which may be replayed at any time and on any stream, so that it must
  *     not share the stream's buffer), the call runs without the split (same result up to summation
