@@ -387,21 +387,31 @@ __global__ __launch_bounds__(256) void paged_prefix_merge_kernel(const float* __
   const bool there = query < queries;
   const int64_t q = there ? query : queries - 1;
   const int first = seq_lens[q / Hq] >= P ? 0 : pre_parts;
-  const float *so = part_o + q * parts * D + d, *ss = part_s + q * parts * 2;
-  float M = -__builtin_inff();
-  for (int i = first; i < parts; ++i) M = __builtin_fmaxf(M, ss[2 * i]);
-  const float ref = M == -__builtin_inff() ? 0.f : M;
+  // lane i: maximum and sum of part i (at most 64), none if it is not to be read or had no keys (NaN scores leave a maximum of -inf too, but a sum of NaN)
+  const int lane = tid & 63;
+  float mi = -__builtin_inff(), si = 0.f;
+  if (lane >= first && lane < parts) {
+    mi = part_s[(q * parts + lane) * 2];
+    si = part_s[(q * parts + lane) * 2 + 1];
+  }
+  const unsigned long long some = __ballot(!(mi == -__builtin_inff() && si == 0.f));
+  const float M = wave_max(mi), ref = M == -__builtin_inff() ? 0.f : M, wi = __builtin_amdgcn_exp2f(mi - ref);
+  const float* so = part_o + q * parts * D + d;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float S = 0.f;
-#pragma unroll 4
-  for (int i = first + grp; i < parts; i += 4) {
-    const float mi = ss[2 * i], w = __builtin_amdgcn_exp2f(mi - ref);
-    const f32x4 x = *reinterpret_cast<const f32x4_mem*>(so + (int64_t)i * D);
-    const float si = ss[2 * i + 1];
-    if (!(mi == -__builtin_inff() && si == 0.f)) {       // (else: no keys. NaN scores leave a maximum of -inf too, but a sum of NaN)
-      S += si * w;
+  for (int i0 = grp; i0 < parts; i0 += 16) {             // four parts of a group's turn at once
+    f32x4 x[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] += x[e] * w;
+    for (int k = 0; k < 4; ++k) x[k] = *reinterpret_cast<const f32x4_mem*>(so + (int64_t)(i0 + 4 * k < parts ? i0 + 4 * k : i0) * D);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = i0 + 4 * k;
+      const float w = __shfl(wi, i), s = __shfl(si, i);
+      if (i < parts && (some >> i & 1)) {
+        S += s * w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += x[k][e] * w;
+      }
     }
   }
   __shared__ f32x4 buf[256];

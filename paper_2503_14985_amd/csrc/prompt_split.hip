@@ -51,18 +51,31 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptKernel p, const 
   if (b < 0) return;
   b = uniform(b);
   seq.get(p.items, b);
-  const float *so = part_o + q * parts * D + lane * E, *ss = part_s + q * parts * 2;
-  float M = -__builtin_inff();
-  for (int i = 0; i < parts; ++i) M = __builtin_fmaxf(M, ss[2 * i]);
-  const float ref = M == -__builtin_inff() ? 0.f : M;
+  // lane i: maximum and sum of part i (at most 16); none where the part had no keys (NaN scores leave a maximum of -inf too, but a sum of NaN)
+  float mi = -__builtin_inff(), si = 0.f;
+  if (lane < parts) {
+    mi = part_s[(q * parts + lane) * 2];
+    si = part_s[(q * parts + lane) * 2 + 1];
+  }
+  const unsigned long long some = __ballot(!(mi == -__builtin_inff() && si == 0.f));
+  const float M = wave_max(mi), ref = M == -__builtin_inff() ? 0.f : M, wi = __builtin_amdgcn_exp2f(mi - ref);
+  const float* so = part_o + q * parts * D + lane * E;
   float acc[E] = {}, S = 0.f;
-#pragma unroll 4
-  for (int i = 0; i < parts; ++i) {
-    const float mi = ss[2 * i], si = ss[2 * i + 1], w = __builtin_amdgcn_exp2f(mi - ref);
-    if (mi == -__builtin_inff() && si == 0.f) continue;  // (no keys; NaN scores leave a sum of NaN)
-    S += si * w;
+  for (int i0 = 0; i0 < parts; i0 += 8) {
+    float x[8][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] += so[(int64_t)i * D + e] * w;
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[k][e] = so[(int64_t)(i0 + k < parts ? i0 + k : i0) * D + e];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float w = __shfl(wi, i0 + k), s = __shfl(si, i0 + k);
+      if (some >> (i0 + k) & 1) {
+        S += s * w;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += x[k][e] * w;
+      }
+    }
   }
   float sum = 0.f;
 #pragma unroll
