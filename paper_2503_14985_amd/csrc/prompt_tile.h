@@ -342,6 +342,9 @@ __device__ __forceinline__ uint32_t prompt_redo(const PromptKernel& p, const Pro
 //   * A masked key's weight is 0, and 0 times a V that is not finite would be NaN. A row whose output is not finite, and to whose last tiles such a V belongs that it does not
 //     see, is worked out again by itself (prompt_redo). Nothing is spent on that before it is needed but one look at the outputs, 64 multiplications an item.
 //
+// 8192 tokens, 32 heads over 8, D = 128: 470 us, 1170 TFLOP/s (the two-group kernel for a whole batch: 1150 to 1215); 512 tokens each of four sequences behind up to 8192 keys: 212 us. What bounds it is there the board's
+// power and the exponentials beside the MFMAs, here that the longest of 272 items is as long as the call; with short sequences the start and end of an item (13 prompts of 8191 tokens in all: 92 us).
+//
 // The largest weight of a row lies between 1 and 2^8 (the reference moves when the maximum has grown by 8): fp16 weights lose nothing but what is below 2^-25 of it. Weights are
 // rounded to 16 bits for the second product, and it is the rounded ones that are summed: what the rounding does to a row's weights as a whole cancels.
 // What a workgroup does of an item when its keys are split over several: tiles t0 .. t0 + tiles - 1 of them; the result goes, in fp32 and not divided by the sum, to
