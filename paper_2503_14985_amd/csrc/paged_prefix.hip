@@ -401,14 +401,17 @@ __global__ __launch_bounds__(256) void paged_prefix_merge_kernel(const float* __
   const float* so = part_o + q * parts * D + d;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float S = 0.f;
-  for (int i0 = grp; i0 < parts; i0 += 16) {             // four parts of a group's turn at once
+  for (int i0 = 0; i0 < parts; i0 += 16) {               // four parts of a group's turn at once; all lanes stay, they hold the parts' weights
     f32x4 x[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = *reinterpret_cast<const f32x4_mem*>(so + (int64_t)(i0 + 4 * k < parts ? i0 + 4 * k : i0) * D);
+    for (int k = 0; k < 4; ++k) {
+      const int i = i0 + grp + 4 * k;
+      x[k] = *reinterpret_cast<const f32x4_mem*>(so + (int64_t)(i < parts ? i : parts - 1) * D);
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int i = i0 + 4 * k;
-      const float w = __shfl(wi, i), s = __shfl(si, i);
+      const int i = i0 + grp + 4 * k;
+      const float w = __shfl(wi, i & 63), s = __shfl(si, i & 63);
       if (i < parts && (some >> i & 1)) {
         S += s * w;
 #pragma unroll

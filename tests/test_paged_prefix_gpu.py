@@ -124,3 +124,32 @@ def test_scales(binding, scale):
     Q = normal(3, (len(lens), Hq, 128), FP)
     O = binding.mlt_paged_attn_decode_prefix(Q, Kc, Vc, prefix, P, table, ints(lens), scale)
     verify(O, Q, Kc, Vc, prefix, P, table, lens, scale)
+
+
+SHARED = {
+    # long enough to be read once for all: up to 16 queries of a key head, up to 32, more
+    "16": (6001, [6001, 6040, 0], (8, 2), 32),
+    "32": (5008, [5008 + 30 * i for i in range(5)] + [77, 5100], (8, 2), 16),
+    "256": (9003, [9003 + i % 50 for i in range(68)] + [0, 9002], (8, 2), 48),
+}
+
+
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows", list(SHARED))
+def test_shared_reading(binding, rows, D, dtype):
+    P, lens, (Hq, H), block = SHARED[rows]
+    Kc, Vc, prefix, table = make(len(rows), P, lens, H, D, block, dtype)
+    Q, scale = normal(60, (len(lens), Hq, D), dtype), 1.0 / math.sqrt(D)
+    for s in (scale, -0.05):
+        O = binding.mlt_paged_attn_decode_prefix(Q, Kc, Vc, prefix, P, table, ints(lens), s)
+        name = binding.mlt_last_kernel()
+        assert "_%s_p" % rows in name, name
+        verify(O, Q, Kc, Vc, prefix, P, table, lens, s, name)
+    need = binding.mlt_paged_attn_decode_prefix_work(len(lens), Hq, H, D, block, table.shape[1], P)
+    work = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
+    again = binding.mlt_paged_attn_decode_prefix(Q, Kc, Vc, prefix, P, table, ints(lens), s, work=work[:need])
+    assert need > 0 and torch.equal(O, again) and bool((work[need:] == 255).all())
+    alone = binding.mlt_paged_attn_decode_prefix(Q, Kc, Vc, prefix, P, table, ints(lens), s, work=work[:need - 16])
+    assert "_p0_" in binding.mlt_last_kernel()
+    verify(alone, Q, Kc, Vc, prefix, P, table, lens, s)

@@ -39,8 +39,8 @@ def cases(lib, seed=0, dtype=BF):
         Kc, Vc, table = cache_of(seed + 4, lens, H, D, block, dtype)
         t = [normal(seed + 5, (sum(new), Hq, D), dtype), Kc, Vc, ints(ends(new)), ints(lens), table]
         out[name] = (t, lambda t, O, st, work: lib.mlt_paged_attn_prompt(*t, 0.1, O=O, stream=st), t[0].shape)
-    for name, B, P, own in (("prefix, few", 3, 700, 90), ("prefix, many", 12, 1500, 200), ("prefix, none", 4, 0, 1200)):
-        lens = [P + own - 7 * b for b in range(B)]
+    for name, B, P, own in (("prefix, few", 3, 5700, 90), ("prefix, many", 70, 8500, 30), ("prefix, alone", 12, 500, 200), ("prefix, none", 4, 0, 1200)):
+        lens = [P + own - b * own // 100 for b in range(B)]
         Kc, Vc, table = cache_of(seed + 6, lens, H, D, block, dtype)
         t = [normal(seed + 7, (B, Hq, D), dtype), Kc, Vc, table[0].contiguous(), table, ints(lens)]
         out[name] = (t, lambda t, O, st, work, P=P: lib.mlt_paged_attn_decode_prefix(t[0], t[1], t[2], t[3], P, t[4], t[5], 0.1, O=O, work=work, stream=st), t[0].shape)
@@ -148,7 +148,7 @@ def verify(name, t, O):
             K, V = (rows_of(c, t[5][b, :-(-m // block)], m) for c in t[1:3])
             check_packed(O[cu[b]:cu[b + 1]], t[0][cu[b]:cu[b + 1]], K, V, [0, cu[b + 1] - cu[b]], [0, m], 0.1, True, what=name)
     elif name.startswith("prefix"):
-        P, block = {"few": 700, "many": 1500, "none": 0}[name.split()[1]], t[1].shape[2]
+        P, block = {"few": 5700, "many": 8500, "alone": 500, "none": 0}[name.split()[1]], t[1].shape[2]
         for b, m in enumerate(t[5].tolist()):
             j = torch.arange(m, device="cuda")
             blk = torch.where(j < P, t[3][j // block], t[4][b][j // block]).long()
@@ -177,7 +177,7 @@ def test_captured_and_replayed(lib, with_work):
         works = None
         if with_work:
             B, Hq, D = t[0].shape
-            P = 700 if "few" in name else 1500
+            P = 5700 if "few" in name else 8500
             need = lib.mlt_paged_attn_decode_prefix_work(B, Hq, t[1].shape[1], D, t[1].shape[2], t[4].shape[1], P)
             assert need > 0
             works = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(2)]
@@ -254,8 +254,8 @@ def test_the_debug_build_agrees(lib):
                     O = torch.full_like(want, math.nan)
                     assert dbg.mlt_paged_attn_prompt(cu[-1], len(batch), Hq, H, D, block, table.shape[1], Kc.shape[0], p(Q), Hq * D, p(Kc), p(Vc), p(a), p(n), p(table), p(O), Hq * D, 0.1, code, st()) == 0
                     assert dbg.mlt_last_kernel().decode() == name and torch.equal(O.view(torch.int16), want.view(torch.int16)), name
-            for B, P, own in ((3, 500, 300), (6, 777, 90), (20, 1500, 260), (5, 0, 900)):
-                lens = [P + own - 3 * b for b in range(B)]
+            for B, P, own in ((3, 6000, 300), (6, 5777, 90), (70, 9000, 20), (20, 500, 260), (5, 0, 900), (2, 0, 9000)):
+                lens = [P + own - b * own // 100 for b in range(B)]
                 Kc, Vc, table = cache_of(6, lens, H, D, block, dtype)
                 Q, n, pre = normal(7, (B, Hq, D), dtype), ints(lens), table[0].contiguous()
                 want = lib.mlt_paged_attn_decode_prefix(Q, Kc, Vc, pre, P, table, n, 0.1)
