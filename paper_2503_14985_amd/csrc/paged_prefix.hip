@@ -11,8 +11,8 @@
 //     transposing LDS read fetches V for the same keys. P goes in as the sum of two 16-bit numbers, itself rounded and what that left (16 bits of bf16, 22 of fp16): the matrix
 //     units have time for it. Its sum is taken in fp32 before the rounding.
 // 64 sequences, 32 heads over 8, D = 128, behind a prefix of 8192 with up to 512 own keys: 35 us (29 here, of which a third is the partial results of 17 ranges; 6 in joining them); 250 behind 32001: 151 us, the
-// rate of the prompts' kernel; 64 behind 1024 with up to 4096 own keys: 122 us, 5.5 TB/s. Ranges of 8 key tiles at least: with 4 the first takes 53 us, with 12 35, but 16 sequences behind 4096 keys 25 instead of 21.
-// A sequence that ends inside the prefix is not part of it: all of its keys, up to its end, are its own, read through the prefix's table. So are they where there is no room for
+// rate of the prompts' kernel; 64 behind 1024 with up to 4096 own keys: 120 us, 5.6 TB/s. Ranges of 8 key tiles at least: with 4 the first takes 53 us, with 12 35, but 16 sequences behind 4096 keys 25 instead of 21.
+// Short prefixes are not shared at all (plan_prefix). A sequence that ends inside the prefix is not part of it: all of its keys, up to its end, are its own, read through the prefix's table. So are they where there is no room for
 // partial results.
 #include <stdio.h>
 
@@ -438,32 +438,57 @@ __global__ __launch_bounds__(256) void paged_prefix_merge_kernel(const float* __
 
 struct PrefixPlan { int pre, pre_parts, pre_per, pre_tiles, own_parts, waves; };
 
+// What a plan takes, in us, as far as one can tell from the largest lengths: `blocks` workgroups in rounds, each of some start and end and of its wavefronts' units one after the other; fitted to 1 to 250
+// sequences with 300 to 32000 keys in front and 64 to 8192 of their own.
+double px_time(int64_t blocks, int64_t units, int64_t D, int64_t ncu) {
+  const int64_t places = D == 64 ? 2 * ncu : ncu;
+  return (double)((blocks + places - 1) / places) * (2.5 + (D == 64 ? 0.7 : 1.3) * (double)units);
+}
+
+// Wavefronts of an item of own keys, and into how many ranges those are cut, for `left` units of 32 keys beside `others` workgroups; merged: there is a second kernel anyway. 512 items of 17 units beside 128 workgroups
+// with 2, 4, 8 wavefronts: 37.4, 39.6, 40.9 us in all; 512 of 129: 171, 128, 123.
+double plan_own(PrefixPlan& p, int64_t items, int64_t left, int64_t others, bool merged, int64_t D, int64_t ncu) {
+  double best = 0.;
+  for (int w = 8; w >= 2; w /= 2)
+    for (int n = 1; n <= PX_MAX_PARTS / 2 && (n == 1 || (n * 2 * w <= left && items * n <= 4 * ncu)); n *= 2) {
+      const double t = px_time((items * n * w + PX_NW - 1) / PX_NW + others, (left + w * n - 1) / (w * n), D, ncu) + (n > 1 ? 0.1 * n + (merged ? 0. : 3.5) : 0.);
+      if (best == 0. || t < best) {
+        best = t;
+        p.waves = w;
+        p.own_parts = n;
+      }
+    }
+  return best;
+}
+
+double larger(double x, double y) { return x > y ? x : y; }
+
 PrefixPlan plan_prefix(const PrefixArgs& a, int64_t ncu) {
   PrefixPlan p{0, 0, 0, 0, 1, 8};
   const int64_t G = a.Hq / a.H, rows = a.B * G, tiles = (G + 15) / 16, own = a.max_blocks * a.block_size - a.prefix_len;
   const int64_t items = a.B * a.H * tiles, units = (own + 31) / 32 + 1;
-  if (a.prefix_len > 0 && a.B > 1) {
-    p.pre = rows <= 16 ? 1 : rows <= 32 ? 2 : 3;
-    const int64_t step = p.pre == 3 ? 64 : 32 * PX_NW, steps = (a.prefix_len + step - 1) / step;   // a key tile; a unit for every wavefront
-    p.pre_tiles = p.pre == 3 ? (int)((rows + 255) / 256) : 1;
-    int64_t n = ncu / (a.H * p.pre_tiles);
-    const int64_t least = p.pre == 3 ? 8 : 1;
-    if (n > steps / least) n = steps / least;
-    if (n > PX_MAX_PARTS / 2) n = PX_MAX_PARTS / 2;
-    if (n < 1) n = 1;
-    const int64_t per = (steps + n - 1) / n;
-    p.pre_parts = (int)((steps + per - 1) / per);
-    p.pre_per = (int)(p.pre == 3 ? per : per * PX_NW);
-  }
-  const int64_t left = p.pre ? units : units + (a.prefix_len + 31) / 32;
-  // wavefronts of an item: some 8 to 16 units each, and more of them while there are few items (the first two cases above with 2, 4, 8: 37.4, 39.6, 40.9 us and, of 64 x 4096 own keys, 171, 128, 123)
-  p.waves = left <= 34 ? 2 : left <= 68 ? 4 : 8;
-  while (p.waves < 8 && items * p.waves < ncu) p.waves *= 2;
-  int64_t n = 2 * ncu / items;
-  if (n > left / (2 * p.waves)) n = left / (2 * p.waves);
+  const int64_t pre_units = (a.prefix_len + 31) / 32;
+  const double unit = (double)(items * 128 * a.D) * 1e-6;            // MB of a unit of all items: own keys come at 5 TB/s, the prefix's, read by all, mostly from the L2
+  const double alone = larger(plan_own(p, items, units + pre_units, 0, false, a.D, ncu), unit * ((double)units / 5. + (double)pre_units / 12.));
+  if (a.prefix_len == 0 || a.B == 1) return p;
+  // the prefix once for all
+  PrefixPlan q{0, 0, 0, 0, 1, 8};
+  q.pre = rows <= 16 ? 1 : rows <= 32 ? 2 : 3;
+  const int64_t step = q.pre == 3 ? 64 : 32 * PX_NW, steps = (a.prefix_len + step - 1) / step;     // a key tile; a unit for every wavefront
+  q.pre_tiles = q.pre == 3 ? (int)((rows + 255) / 256) : 1;
+  int64_t n = ncu / (a.H * q.pre_tiles);
+  const int64_t least = q.pre == 3 ? 8 : 1;
+  if (n > steps / least) n = steps / least;
   if (n > PX_MAX_PARTS / 2) n = PX_MAX_PARTS / 2;
-  p.own_parts = n < 1 ? 1 : (int)n;
-  return p;
+  if (n < 1) n = 1;
+  const int64_t per = (steps + n - 1) / n, blocks = (steps + per - 1) / per * q.pre_tiles * a.H;
+  q.pre_parts = (int)((steps + per - 1) / per);
+  q.pre_per = (int)(q.pre == 3 ? per : per * PX_NW);
+  const double theirs = larger(plan_own(q, items, units, blocks, true, a.D, ncu), unit * (double)units / 5.);
+  const double shared = q.pre == 3 ? (4. + (a.D == 64 ? 0.9 : 1.7) * (double)per) * (double)((blocks + ncu - 1) / ncu) : px_time(blocks, per, a.D, ncu);
+  // Every sequence reads the prefix by itself, in one launch, where that is not slower: 16 sequences behind 500 keys 7.7 us (16.9 shared), 32 behind 1000 11.3 (18.8), 64 behind 500 13.9 (23.2),
+  // but 4 behind 1000 9.8 (9.1), 8 behind 2000 13.5 (12.8), and 128 behind 300 are taken for 22.2 shared, 19.1 alone.
+  return alone <= larger(theirs, shared) + (q.pre == 3 ? 5. : 4.2) ? p : q;
 }
 int64_t work_of(const PrefixArgs& a, const PrefixPlan& p) {
   const int64_t parts = p.pre_parts + p.own_parts;
@@ -530,10 +555,7 @@ int run_paged_prefix(const PrefixArgs& a, hipStream_t s, char* name, size_t size
   if (need > 0) {
     work = a.work ? (a.work_bytes >= need ? a.work : nullptr) : cached_scratch(need, s);
     if (!work) {                                         // everything to one item for each sequence and head
-      p = plan_prefix(a, cus());
-      p.pre = p.pre_parts = p.pre_per = p.pre_tiles = 0;
-      p.own_parts = 1;
-      p.waves = 8;
+      p = PrefixPlan{0, 0, 0, 0, 1, 8};
     }
   }
   static const char* const kinds[4] = {"", "_16", "_32", "_256"};
