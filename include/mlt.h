@@ -315,7 +315,7 @@ int mlt_paged_attn_prompt(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D
 
 /*
  * mlt_paged_attn_decode for a batch whose sequences begin with the same prefix_len tokens, with Hq / H query heads to each key/value head. The prefix's
- * keys and values are read once for all sequences:
+ * keys and values are read once for all sequences (by each of them where they are too few for that to pay):
  *   o = sum_j softmax_j(scale * q . k_j) v_j,   j = 0 .. seq_lens[b] - 1,   0 <= seq_lens[b] <= max_blocks * block_size
  *   Q, O           device, contiguous [B, Hq, D]
  *   Kc, Vc, block_size, max_blocks, num_blocks   as for mlt_paged_attn_decode
