@@ -400,9 +400,10 @@ int run_gemm_4bit(const Gemm4bitArgs& g, hipStream_t s, char* name, size_t size)
   if (parts > 1) {
     a.part = cached_scratch(parts * g.M * g.N * 4, s);
     if (a.part) a.counter = scratch_counters(a.part);
-    else parts = 1;
   }
-  if (tile && !a.part && g.M <= 2 * W4_ROWS && nwg * nz * 4 <= ncu) {
+  const bool denied = parts > 1 && !a.part;
+  if (denied) parts = 1;
+  if (tile && denied && g.M <= 2 * W4_ROWS && nwg * nz * 4 <= ncu) {
     // Nothing to split with and tiles for a quarter of the CUs: the rows 32 at a time, by all CUs. Recorded into a graph, as tiles and so: 57 x 4100 x 14336 132 and 90 us,
     // 64 x 8192 x 8192 74 and 47 (three times 32 rows come to the same, four to more).
     for (int64_t r = 0; r < g.M; r += W4_ROWS) {

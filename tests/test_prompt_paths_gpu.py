@@ -122,8 +122,9 @@ def test_calls_are_ordered_behind_the_streams_work(lib, explicit):
 
 def test_two_streams_at_once(lib):
     """Calls on two streams at a time, each with other inputs: partial results and counters of one are not the other's."""
-    for name in cases(lib):
-        a, b = (cases(lib, seed)[name] for seed in (0, 50))
+    ones, others = cases(lib, 0), cases(lib, 50)
+    for name in ones:
+        a, b = ones[name], others[name]
         want = [run(c) for c in (a, b)]
         streams = [torch.cuda.Stream() for _ in range(2)]
         torch.cuda.synchronize()
@@ -167,13 +168,12 @@ def verify(name, t, O):
 @pytest.mark.parametrize("with_work", [False, True], ids=["no_work", "work"])
 def test_captured_and_replayed(lib, with_work):
     """Each call recorded into a graph of its own, replayed several times among eager calls of the same and other inputs on the same and another stream."""
-    stream = torch.cuda.Stream()
+    stream, others = torch.cuda.Stream(), cases(lib, 70)
     for name, case in cases(lib).items():
-        if with_work != ("prefix, few" in name or "prefix, many" in name):
-            if with_work:
-                continue
+        if with_work and name not in ("prefix, few", "prefix, many"):
+            continue
         t, call, shape = case
-        other = cases(lib, 70)[name]
+        other = others[name]
         works = None
         if with_work:
             B, Hq, D = t[0].shape
