@@ -74,6 +74,11 @@ template <typename Tag, int NT> __device__ __forceinline__ void w4_add_parts(con
   }
 }
 
+// Scales and zero points of a chunk of 128 (gemm_4bit_tile.hip): lanes 16 g .. 16 g + 15 of a wavefront load those of its group w4t_group(g), lanes to spare those of its last group again, where the
+// matrix has that group. The last chunk of a row may have fewer (K is a multiple of 32): a group that is not there is not read, whichever lanes would read it.
+template <int G> __host__ __device__ __forceinline__ constexpr int w4t_group(int g) { return g < 128 / G ? g : 128 / G - 1; }
+template <int G> __host__ __device__ __forceinline__ constexpr bool w4t_group_there(int k0, int g, int last_group) { return k0 / G + w4t_group<G>(g) <= last_group; }
+
 // gemm_4bit_tile.hip: nwg workgroups of up to 8 or 16 blocks of 16 columns for every 64 rows and each part of K
 constexpr int W4T_ROWS = 64;
 int run_w4_tile(const W4& a, int dtype, int group, int blocks, unsigned nwg, int parts, hipStream_t s);

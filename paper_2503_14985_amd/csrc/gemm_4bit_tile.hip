@@ -53,7 +53,7 @@ __global__ __launch_bounds__(W4T_NT, 2) void gemm_4bit_tile_kernel(W4 a) {
     va[j] = (uint32_t)(row < M ? row : M - 1) * (uint32_t)a.lda * 2u + (uint32_t)((lane & 15) ^ (row & 15)) * 16u;
   }
   // The wavefront's blocks are wave and wave + 8; a block or column that is not there is the last one again and not written
-  const int w_row = lane >> 2, w_chunk = (lane & 3) ^ (w_row >> 2), s_group = g < NG ? g : NG - 1;
+  const int w_row = lane >> 2, w_chunk = (lane & 3) ^ (w_row >> 2), s_group = w4t_group<G>(g);
   uint32_t vw[CB], vs[CB], vz[CB];
 #pragma unroll
   for (int c = 0; c < CB; ++c) {
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(W4T_NT, 2) void gemm_4bit_tile_kernel(W4 a) {
       if (ZP) load_lds_u8(f_z, vz[c], at + 1280u);
     } else {
       load_lds16_stream(f_w, w_chunk * 32 < left ? vw[c] : vw[c] - (uint32_t)w_chunk * 16u, at);
-      const bool there = k0 / G + g <= last_group || g >= NG;
+      const bool there = w4t_group_there<G>(k0, g, last_group);
       if (there) load_lds_u16(f_s, vs[c], at + 1024u);
       else *(MLT_LDS uint32_t*)(uintptr_t)(at + 1024u + lane * 4u) = 0u;
       if (ZP) {
