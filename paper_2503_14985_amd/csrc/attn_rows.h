@@ -53,7 +53,7 @@ __device__ __forceinline__ void attend_row(const uint16_t* q, uint16_t* out, int
     if (__all(lost)) break;
   }
 #pragma unroll
-  for (int e = 0; e < E; ++e) out[e * 64 + lane] = Elem<Tag>::from_f32(end > 0 ? o[e] / l : 0.f);
+  for (int e = 0; e < E; ++e) out[e * 64 + lane] = Elem<Tag>::from_f32(l == 0.f ? o[e] * 0.f : o[e] / l);   // (no key, or none with a weight: scores of -inf)
 }
 
 }  // namespace mlt
