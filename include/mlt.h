@@ -23,7 +23,7 @@
  *     keys) and mlt_paged_attn_decode_prefix (unless it is given `work`) may spread one result over several workgroups and then keep fp32 partial results in a
  *     scratch buffer, one per (device, stream), allocated with hipMalloc at the first call that
  *     needs it, grown by doubling from 4 MiB (64 MiB covers every split the library chooses by
- *     itself, but for shared prefixes of very large batches) and kept until the process ends. Calls on one stream are ordered by the stream; calls
+ *     itself, but for shared prefixes of very large batches) and kept until the process ends. Calls on one stream are ordered by the stream, whichever threads make them; calls
  *     on different streams use different buffers (on hipStreamPerThread: of different threads). If the allocation fails, or the stream is
  *     recording into a graph (which may be replayed at any time and on any stream, so that it must
  *     not share the stream's buffer), the call runs without the split (same result up to summation

@@ -561,6 +561,16 @@ float* cached_scratch(int64_t bytes, hipStream_t s) {
   return slot->ptr;
 }
 
+// One mutex for the streams of a place in a small table (two streams that share one wait for each other's launches to be enqueued, no more).
+float* cached_scratch(int64_t bytes, hipStream_t s, ScratchTurn& turn) {
+  static std::mutex turns[64];
+  const uintptr_t at = reinterpret_cast<uintptr_t>(s);
+  std::unique_lock<std::mutex> lock(turns[(at >> 4 ^ at >> 12) % 64]);
+  float* p = cached_scratch(bytes, s);
+  if (p) turn.lock_ = std::move(lock);
+  return p;
+}
+
 // The scratch of the entry point that may not allocate (mlt_gemm_noalloc): a fixed array in
 // device memory, one copy per GPU the library runs on, held until the process ends. In host code
 // the array's name is only a handle; its device address is looked up once per device, with that
@@ -590,8 +600,9 @@ int run_gemm(const GemmArgs& g_in, GemmPlan& p, hipStream_t s) {
   GemmArgs g = g_in;
   g.parts = p.parts;
   bool own = false;
+  ScratchTurn turn;
   if (p.parts > 1 && !g.scratch) {
-    g.scratch = cached_scratch(p.scratch_bytes, s);
+    g.scratch = cached_scratch(p.scratch_bytes, s, turn);
     if (g.scratch) {
       g.counters = scratch_counters(g.scratch);
     } else {

@@ -397,8 +397,9 @@ int run_gemm_4bit(const Gemm4bitArgs& g, hipStream_t s, char* name, size_t size)
     while (parts < 8 && rows * 4 * ncu > g.N * parts * 2 && pieces >= 2 * parts * W4_NW) parts *= 2;
   }
   while (parts > 1 && (parts * g.M * g.N * 4 > (int64_t)32 << 20 || (!tile && ncu / parts > kScratchCounters))) parts /= 2;
+  ScratchTurn turn;
   if (parts > 1) {
-    a.part = cached_scratch(parts * g.M * g.N * 4, s);
+    a.part = cached_scratch(parts * g.M * g.N * 4, s, turn);
     if (a.part) a.counter = scratch_counters(a.part);
   }
   const bool denied = parts > 1 && !a.part;

@@ -662,8 +662,9 @@ int run_fp8_t(const GemmFp8Args& a, hipStream_t s, char* name, size_t size) {
   Fp8Plan p = plan_fp8(a, 8, ncu);
   if (p.parts == 0) return MLT_ERR_UNSUPPORTED;          // more workgroups than a launch can have, whatever the tile
   float* part = nullptr;
+  ScratchTurn turn;
   if (p.parts > 1) {
-    part = cached_scratch(part_bytes(p, a), s);
+    part = cached_scratch(part_bytes(p, a), s, turn);
     if (!part) p = plan_fp8(a, 1, ncu);                  // no scratch to be had: the best of the plain forms
   }
   const char* tile = p.variant == GEMM_SKINNY ? "skinny" : p.variant == GEMM_256_PP16 ? "256x256_pp" : p.variant == GEMM_128_PP16 ? "128x128_pp" : p.variant == GEMM_256X128_KP ? "256x128_kp"

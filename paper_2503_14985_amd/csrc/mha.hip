@@ -134,8 +134,9 @@ int run_mha(const MhaArgs& a, MhaPlan& p, hipStream_t s) {
   if (!p.supported) return MLT_ERR_UNSUPPORTED;
   if (p.key_groups > 1) {
     float* scratch = nullptr;
+    ScratchTurn turn;
     if (p.nsplit > 1) {
-      scratch = cached_scratch(mha_ks_scratch_bytes(a, p.nsplit), s);
+      scratch = cached_scratch(mha_ks_scratch_bytes(a, p.nsplit), s, turn);
       if (!scratch) p.nsplit = 1;
     }
     return run_mha_ks(a, p.bm, p.nsplit, scratch, s);

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <mutex>
+
 namespace mlt {
 
 enum GemmVariant {
@@ -280,6 +282,13 @@ int run_gemm_4bit(const Gemm4bitArgs& a, hipStream_t s, char* name, size_t size)
 // (and grown by doubling) from call to call, never freed; nullptr if it cannot be had, and while the
 // stream records into a graph. Work of one stream that uses it is ordered by the stream.
 float* cached_scratch(int64_t bytes, hipStream_t s);
+// For calls that enqueue several launches with the scratch between them: where there is scratch to be had, the call has the stream's turn until `turn` goes out of scope, so that another thread's
+// call on the stream cannot enqueue a launch that writes the same scratch in between.
+class ScratchTurn {
+  std::unique_lock<std::mutex> lock_;
+  friend float* cached_scratch(int64_t bytes, hipStream_t s, ScratchTurn& turn);
+};
+float* cached_scratch(int64_t bytes, hipStream_t s, ScratchTurn& turn);
 bool stream_is_capturing(hipStream_t s);   // true while `s` records into a graph
 
 }  // namespace mlt

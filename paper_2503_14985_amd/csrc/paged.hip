@@ -387,8 +387,9 @@ int plan_paged_split(const PagedArgs& a) {
 int run_paged_decode(const PagedArgs& a, hipStream_t s, int* nsplit_out) {
   int nsplit = plan_paged_split(a);
   float* part = nullptr;
+  ScratchTurn turn;
   if (nsplit > 1) {
-    part = cached_scratch(a.B * a.H * nsplit * (2 + a.D) * (int64_t)sizeof(float), s);
+    part = cached_scratch(a.B * a.H * nsplit * (2 + a.D) * (int64_t)sizeof(float), s, turn);
     if (!part) nsplit = 1;                               // no scratch to be had: the plain form
   }
   if (nsplit_out) *nsplit_out = nsplit;

@@ -514,8 +514,9 @@ int run_paged_fp8(const PagedFp8Args& a, hipStream_t s, int* nsplit_out, int* wa
   int nsplit = plan_paged_fp8_split(a, a.B * a.H * tiles, ncu);
   if (!launch_fits(a.B * a.Hq, 256)) nsplit = 1;         // (what the merging kernel would need)
   float* part = nullptr;
+  ScratchTurn turn;
   if (nsplit > 1) {
-    part = cached_scratch(a.B * a.Hq * nsplit * (2 + a.D) * (int64_t)sizeof(float), s);
+    part = cached_scratch(a.B * a.Hq * nsplit * (2 + a.D) * (int64_t)sizeof(float), s, turn);
     if (!part) nsplit = 1;                               // no scratch to be had: the plain form
   }
   const int64_t wgs = a.B * a.H * tiles * nsplit;

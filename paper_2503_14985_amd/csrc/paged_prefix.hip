@@ -552,8 +552,9 @@ int run_paged_prefix(const PrefixArgs& a, hipStream_t s, char* name, size_t size
   PrefixPlan p = plan_prefix(a, cus());
   const int64_t need = work_of(a, p);
   float* work = nullptr;
+  ScratchTurn turn;
   if (need > 0) {
-    work = a.work ? (a.work_bytes >= need ? a.work : nullptr) : cached_scratch(need, s);
+    work = a.work ? (a.work_bytes >= need ? a.work : nullptr) : cached_scratch(need, s, turn);
     if (!work) {                                         // everything to one item for each sequence and head
       p = PrefixPlan{0, 0, 0, 0, 1, 8};
     }

@@ -60,7 +60,8 @@ int run_prompt(const PromptArgs& a, hipStream_t s, char* name, size_t size) {
   int64_t parts = ncu / items_guess < 16 ? ncu / items_guess : 16;
   if (parts > longest / kPromptPart) parts = longest / kPromptPart;
   float* scratch = nullptr;
-  if (parts > 1) scratch = cached_scratch(a.T * a.Hq * parts * (a.D + 2) * 4, s);
+  ScratchTurn turn;
+  if (parts > 1) scratch = cached_scratch(a.T * a.Hq * parts * (a.D + 2) * 4, s, turn);
   if (!scratch) parts = 1;
   if (!launch_fits(grid * parts, PA_NT)) return MLT_ERR_UNSUPPORTED;
   float c = (a.scale < 0 ? -a.scale : a.scale) * 1.4426950408889634f;   // c > 0 always, as in launch_mha_pp
