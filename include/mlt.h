@@ -349,8 +349,8 @@ int64_t mlt_paged_attn_decode_prefix_work(int64_t B, int64_t Hq, int64_t H, int6
  * group is 32, 64 or 128; the last one of a row may be shorter. Products and the sum over a group are fp32, as is the sum over the groups, each times its scale; C is
  * rounded once. An infinity in a row of A, or a scale that is infinite, may give NaN in its row, or column. The order of the sums goes by the sizes (and by whether a
  * stream records the call into a graph, which splits nothing); equal calls give equal bits. K a multiple of 32, lda a multiple of 8,
- * ldw of 16, lda below 2^23, ldw below 2^24, lds and ldz below 2^26 (MLT_ERR_UNSUPPORTED); A and Wq 16-byte, S and C 2-byte aligned. Any M is taken; the kernels are made
- * for up to 64 rows (the weights are read again for every 64). M == 0 or N == 0 is a no-op, K == 0 stores zeros.
+ * ldw of 16, lda below 2^23, ldw below 2^24, lds and ldz below 2^26 (MLT_ERR_UNSUPPORTED); A and Wq 16-byte, S and C 2-byte aligned. M is taken up to 64 * 65535
+ * (MLT_ERR_UNSUPPORTED; any with K == 0) as far as a launch has room for its tiles of 64 rows and 128 or 256 columns; the kernels are made for up to 64 rows (the weights are read again for every 64). M == 0 or N == 0 is a no-op, K == 0 stores zeros.
  */
 int mlt_gemm_w4(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, const void* Wq, int64_t ldw, int64_t group, const void* S, int64_t lds,
                 const uint8_t* Z, int64_t ldz, void* C, int64_t ldc, int dtype, void* stream);

@@ -423,7 +423,7 @@ int run_gemm_4bit(const Gemm4bitArgs& g, hipStream_t s, char* name, size_t size)
   }
   a.share = (int)((tile ? blocks : g.N) / nwg);
   a.rest = (int)((tile ? blocks : g.N) % nwg);
-  if (nz > 65535 || !launch_fits(nwg * parts * nz, 512)) return MLT_ERR_UNSUPPORTED;
+  if (nz > kW4MostTiles || !launch_fits(nwg * parts * nz, 512)) return MLT_ERR_UNSUPPORTED;
   snprintf(name, size, "gemm_4bit_g%d_m%d_parts%d", (int)g.group, (int)rows, (int)parts);
   if (tile) return run_w4_tile(a, g.dtype, (int)g.group, (int)wide, (unsigned)nwg, (int)parts, s);
   if (g.dtype == MLT_BF16) return g.Z ? run_w4_t<bf16_tag, true>(a, (int)g.group, (unsigned)nwg, (int)parts, s) : run_w4_t<bf16_tag, false>(a, (int)g.group, (unsigned)nwg, (int)parts, s);

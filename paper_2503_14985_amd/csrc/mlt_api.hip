@@ -568,6 +568,7 @@ int mlt_gemm_w4(int64_t M, int64_t N, int64_t K, const void* A, int64_t lda, con
     if (!aligned(A, 16) || !aligned(Wq, 16) || !aligned(S, 2)) return MLT_ERR_INVALID_ARG;
     if (K % 32 || lda % 8 || ldw % 16) return MLT_ERR_UNSUPPORTED;
     if (lda >= 1 << 23 || ldw >= 1 << 24 || lds >= 1 << 26 || (Z && ldz >= 1 << 26)) return MLT_ERR_UNSUPPORTED;   // 32-bit offsets inside a tile
+    if (M > (int64_t)kW4MostTiles * 64) return MLT_ERR_UNSUPPORTED;
   }
   if (!device_is_gfx950()) return MLT_ERR_DEVICE;
   Gemm4bitArgs a{M, N, K, (const uint16_t*)A, lda, (const uint8_t*)Wq, ldw, group, (const uint16_t*)S, lds, Z, ldz, (uint16_t*)C, ldc, dtype};

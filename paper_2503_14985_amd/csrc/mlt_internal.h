@@ -276,6 +276,7 @@ struct Gemm4bitArgs {
   uint16_t* C; int64_t ldc;
   int dtype;
 };
+constexpr int kW4MostTiles = 65535;   // tiles of 64 rows of a call: the grid's third dimension
 int run_gemm_4bit(const Gemm4bitArgs& a, hipStream_t s, char* name, size_t size);   // gemm_4bit.hip
 
 // The library's own scratch memory for a stream of the current device: at least `bytes`, behind its counters, kept
