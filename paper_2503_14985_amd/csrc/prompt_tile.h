@@ -41,6 +41,11 @@ inline int64_t prompt_grid(const PromptItems& a, int rows) {
   return (tiles * a.heads + a.per_team - 1) / a.per_team * a.nxcd;
 }
 
+// Sequences up to which a workgroup finds its item in the order of the keys (prompt_item) and not in the batch's: it looks at all of them, in every workgroup. us sorted / in the batch's order, 32 heads
+// over 8: 64 single tokens behind up to 4000 keys 97 / 127, 128 159 / 195, 256 355 / 385; but 128 ragged sequences of 16384 tokens 149 / 121, 256 195 / 124, 256 x 32 tokens 120 / 62, 512 x 16 312 / 109,
+// 8192 single tokens 48500 / 1515. (8 to 32 sequences: the batch's order 2 to 17 % faster.)
+constexpr int kPromptSorted = 128;
+
 // rows q_offsets[b] .. of a sequence and its keys, with what is out of range put right
 struct PromptSeq {
   int q0, n, k0, m;
@@ -60,12 +65,37 @@ struct PromptSeq {
   }
 };
 
+// Of more than kPromptSorted sequences: slot by slot in the batch's order. Sequence b has the slots from first(b) = floor(q0 G / ROWS) + b on, of which its tiles need no more than lie before first(b + 1)
+// (floor(x + y) - floor(x) + 1 >= ceil(y)); the last b with first(b) <= slot is found by probes of 64 sequences at once, two rounds for 4096, whatever the offsets hold.
+template <int ROWS>
+__device__ __forceinline__ bool prompt_item_at(const PromptItems& a, int slot, PromptSeq& seq, int& seq_b, int& tile) {
+  const int lane = threadIdx.x & 63;
+  auto first = [&](int b) {
+    const int q = a.q_offsets[b];
+    return (int)((int64_t)(q < 0 ? 0 : q > a.T ? a.T : q) * a.G / ROWS) + b;
+  };
+  int lo = 0, n = a.B;
+  while (n > 1) {
+    const int step = (n + 63) / 64, at = lane * step;
+    const unsigned long long in = __ballot(at < n && first(lo + (at < n ? at : 0)) <= slot);
+    if (!in) return false;                                 // in front of the first sequence
+    const int up = (63 - __builtin_clzll(in)) * step;
+    lo += up;
+    n = n - up < step ? n - up : step;
+  }
+  seq_b = lo;
+  seq.get(a, lo);
+  tile = (int)(((int64_t)seq.n * a.G + ROWS - 1) / ROWS) - 1 - (slot - first(lo));
+  return tile >= 0;
+}
+
 // The item of a workgroup: tile `tile` of the rows of one sequence and key/value head `h`; false: there is none left. The tiles of all sequences are taken in the order of
 // their keys, most first, so that the launch ends with short ones: by the tokens that the tile's last row sees, in 64 steps of the longest sequence, within a step
 // sequence by sequence. A sequence's tiles with at least L keys are its last (m - L) / tokens + 1 (a reciprocal's rounding moves a tile to the next step, the same
 // way in every workgroup). `buf`: 6 * NT ints of LDS, free again afterwards (behind a barrier).
 template <int ROWS, int NT>
 __device__ __forceinline__ bool prompt_item(const PromptItems& a, int* buf, PromptSeq& seq, int& seq_b, int& h, int& tile) {
+  static_assert(kPromptSorted <= NT, "a thread for each sequence");
   const int xcd = (int)blockIdx.x % a.nxcd, idx = (int)blockIdx.x / a.nxcd * a.per_team + xcd / a.teams;
   h = xcd % a.teams * a.heads + idx % a.heads;
   int rank = idx / a.heads;
@@ -76,10 +106,10 @@ __device__ __forceinline__ bool prompt_item(const PromptItems& a, int* buf, Prom
     tile = tiles - 1 - rank;
     return tile >= 0;
   }
+  if (a.B > kPromptSorted) return prompt_item_at<ROWS>(a, rank, seq, seq_b, tile);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   constexpr int NW = NT / 64;                            // (NW * 64 partial counts: NT ints)
   int *mm = buf, *tt = buf + NT, *part = buf + 2 * NT, *nn = buf + 3 * NT, *qq = buf + 4 * NT, *kk = buf + 5 * NT;
-  auto tiles_of = [&](const PromptSeq& s) { return (int)(((int64_t)s.n * a.G + ROWS - 1) / ROWS); };
   // tiles of a sequence with at least L keys; L < 0: all of them
   auto at_least = [&](int m, int tiles, int L) {
     if (L < 0) return tiles;
@@ -89,17 +119,15 @@ __device__ __forceinline__ bool prompt_item(const PromptItems& a, int* buf, Prom
   };
   // the longest sequence
   int longest = 0;
-  for (int b = tid; b < a.B; b += NT) {
+  if (tid < a.B) {
     PromptSeq s;
-    s.get(a, b);
-    if (s.n > 0 && s.m > longest) longest = s.m;
-    if (a.B <= NT) {                                     // all there are: kept
-      mm[tid] = s.m;
-      tt[tid] = tiles_of(s);
-      nn[tid] = s.n;
-      qq[tid] = s.q0;
-      kk[tid] = s.k0;
-    }
+    s.get(a, tid);
+    if (s.n > 0) longest = s.m;
+    mm[tid] = s.m;
+    tt[tid] = (int)(((int64_t)s.n * a.G + ROWS - 1) / ROWS);
+    nn[tid] = s.n;
+    qq[tid] = s.q0;
+    kk[tid] = s.k0;
   }
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) { const int o = __shfl_xor(longest, s); longest = o > longest ? o : longest; }
@@ -111,19 +139,7 @@ __device__ __forceinline__ bool prompt_item(const PromptItems& a, int* buf, Prom
   const int step = longest / 64 + 1;
   // lane k: tiles with at least k * step keys (k = 0: all)
   int count = 0;
-  for (int b0 = 0; b0 < a.B; b0 += NT) {
-    if (a.B > NT) {                                      // these NT sequences
-      PromptSeq s;
-      s.m = 0; s.n = 0;
-      if (b0 + tid < a.B) s.get(a, b0 + tid);
-      __syncthreads();
-      mm[tid] = s.m;
-      tt[tid] = tiles_of(s);
-      __syncthreads();
-    }
-    const int here = a.B - b0 < NT ? a.B - b0 : NT;
-    for (int b = wave; b < here; b += NW) count += at_least(mm[b], tt[b], lane ? lane * step : -1);
-  }
+  for (int b = wave; b < a.B; b += NW) count += at_least(mm[b], tt[b], lane ? lane * step : -1);
   part[wave * 64 + lane] = count;
   __syncthreads();
   count = 0;
@@ -139,18 +155,8 @@ __device__ __forceinline__ bool prompt_item(const PromptItems& a, int* buf, Prom
   if (found) {
     found = false;
     for (int b0 = 0; b0 < a.B; b0 += 64) {               // every wavefront for itself
-      int m = 0, tiles = 0;
-      if (b0 + lane < a.B) {
-        if (a.B <= NT) {
-          m = mm[b0 + lane];
-          tiles = tt[b0 + lane];
-        } else {
-          PromptSeq s;
-          s.get(a, b0 + lane);
-          m = s.m;
-          tiles = tiles_of(s);
-        }
-      }
+      const bool there = b0 + lane < a.B;
+      const int m = there ? mm[b0 + lane] : 0, tiles = there ? tt[b0 + lane] : 0;
       const int above = at_least(m, tiles, hi), mine = at_least(m, tiles, lo) - above;
       int upto = mine;
 #pragma unroll
@@ -168,13 +174,11 @@ __device__ __forceinline__ bool prompt_item(const PromptItems& a, int* buf, Prom
     }
   }
   b = __builtin_amdgcn_readfirstlane(b);
-  if (found && a.B <= NT) {
+  if (found) {
     seq.q0 = uniform(qq[b]);
     seq.n = uniform(nn[b]);
     seq.k0 = uniform(kk[b]);
     seq.m = uniform(mm[b]);
-  } else if (found) {
-    seq.get(a, b);
   }
   seq_b = b;
   __syncthreads();
