@@ -291,10 +291,11 @@ int mlt_paged_attn_decode_fp8(int64_t B, int64_t Hq, int64_t H, int64_t D, int64
  *                sequence b's queries (none, one, many)
  *   k_offsets    device, int32 [B + 1], the same for its keys, up to Tk; may be q_offsets
  *   O            device, `dtype`: Tq rows of Hq heads, row stride ldo. Rows of no sequence are neither read nor written.
- * Weights are rounded to `dtype` before they multiply V, relative to a maximum of their row; their sum is that of the rounded ones. What a query does not see
- * has no influence on it, whatever it holds (infinities and NaN too). Offsets out of their range or order give wrong results for their sequences, but no access out
- * of range. D must be 64 or 128, ldq, ldk, ldv, ldo multiples of 8 (MLT_ERR_UNSUPPORTED); all tensors of `dtype` 16-byte aligned, scale finite,
- * H a divisor of Hq (MLT_ERR_INVALID_ARG). Tq, B or Hq equal to 0 is a no-op.
+ * Weights are rounded to `dtype` before they multiply V, relative to a maximum of their row; their sum is that of the rounded ones (with the output's own rounding, outputs of random
+ * inputs are off by 1.1 to 1.4 times what weights in fp32 would leave). What a query does not see
+ * has no influence on it, whatever it holds (infinities and NaN too); one whose scores are all -inf gives zeros. Offsets out of their range or order give wrong results for their sequences, but no access out
+ * of range. D must be 64 or 128, ldq, ldk, ldv, ldo multiples of 8, ldk and ldv below 2^23, ldo below 2^29, Tq, Tk, B, Hq * D and Tq * Hq / H below 2^29 (MLT_ERR_UNSUPPORTED); all tensors of `dtype`
+ * 16-byte aligned, scale finite, H a divisor of Hq (MLT_ERR_INVALID_ARG). Tq, B or Hq equal to 0 is a no-op.
  */
 int mlt_mha_packed_fwd(int64_t Tq, int64_t Tk, int64_t B, int64_t Hq, int64_t H, int64_t D, const void* Q, int64_t ldq, const void* K, int64_t ldk,
                        const void* V, int64_t ldv, const int32_t* q_offsets, const int32_t* k_offsets, void* O, int64_t ldo, float scale,
@@ -307,7 +308,9 @@ int mlt_mha_packed_fwd(int64_t Tq, int64_t Tk, int64_t B, int64_t Hq, int64_t H,
  *   seq_lens, block_table, Kc, Vc, block_size, max_blocks, num_blocks   as for mlt_paged_append: seq_lens[b] counts the sequence's tokens WITH the
  *                             new ones. The i-th of its n new tokens has position seq_lens[b] - n + i and sees the keys up to there.
  * A position below 0 gives zeros. Only slots below seq_lens[b] are read. Lengths are clamped to 0 .. max_blocks * block_size, block numbers to 0 .. num_blocks - 1 (wrong result
- * for that sequence, no access out of range). Requirements as for mlt_mha_packed_fwd; block_size a multiple of 16 up to 1024.
+ * for that sequence, no access out of range). Requirements as for mlt_mha_packed_fwd; block_size a multiple of 16 up to 1024, max_blocks * block_size below 2^29.
+ * The lengths are the device's, so it is the table's width, max_blocks * block_size, that decides whether few rows are spread over many workgroups: with a table far wider than the batch needs, a call
+ * that is short by itself pays for that (33 tokens without history 8 us, with 32768 slots 13.5). A table cut to the batch's longest sequence avoids it.
  */
 int mlt_paged_attn_prompt(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks, int64_t num_blocks,
                           const void* Q, int64_t ldq, const void* Kc, const void* Vc, const int32_t* offsets, const int32_t* seq_lens,
@@ -327,8 +330,9 @@ int mlt_paged_attn_prompt(int64_t T, int64_t B, int64_t Hq, int64_t H, int64_t D
  *   work           device, 16-byte aligned, work_bytes long: fp32 partial results, needed only while the call runs; or NULL: the library's scratch of the stream. With less than
  *                  mlt_paged_attn_decode_prefix_work says, or NULL on a stream that records into a graph, the prefix is read again for
  *                  every sequence. Two captured graphs that may run at the same time need a work of their own each.
- * Weights of own keys keep about 16 bits or more whatever `dtype`, as do those of the prefix where it is read for up to 32 queries of a key head (B * Hq / H); for more,
- * they are rounded to `dtype`, as in mlt_mha_fwd. An infinity or NaN in a value makes the outputs of the sequences that see it non-finite. The limits of what is read, clamping and requirements are those of mlt_paged_attn_decode_fp8;
+ * How the work is spread goes by the table's width, as for mlt_paged_attn_prompt (64 sequences behind 8192 keys with 512 own ones 35 us, with 32768 slots a sequence 48).
+ * Weights of own keys keep about 16 bits or more whatever `dtype`, as do those of the prefix where it is read for up to 32 queries of a key head (B * Hq / H) or by every sequence for itself; where it is read
+ * once for more, they are rounded to `dtype`, as in mlt_mha_fwd. An infinity or NaN in a value makes the outputs of the sequences that see it non-finite. The limits of what is read, clamping and requirements are those of mlt_paged_attn_decode_fp8;
  * prefix_len must lie in 0 .. max_blocks * block_size (MLT_ERR_INVALID_ARG).
  */
 int mlt_paged_attn_decode_prefix(int64_t B, int64_t Hq, int64_t H, int64_t D, int64_t block_size, int64_t max_blocks, int64_t num_blocks,
@@ -347,8 +351,9 @@ int64_t mlt_paged_attn_decode_prefix_work(int64_t B, int64_t Hq, int64_t H, int6
  *   Z       device, uint8 [ceil(K / group)][N], row stride ldz >= N: z, 0 .. 15; or NULL: z = 8 (ldz unused)
  *   C       device, M x N row-major of `dtype`, row stride ldc >= N; written, never read
  * group is 32, 64 or 128; the last one of a row may be shorter. Products and the sum over a group are fp32, as is the sum over the groups, each times its scale; C is
- * rounded once. An infinity in a row of A, or a scale that is infinite, may give NaN in its row, or column. The order of the sums goes by the sizes (and by whether a
- * stream records the call into a graph, which splits nothing); equal calls give equal bits. K a multiple of 32, lda a multiple of 8,
+ * rounded once. The sum over a group is taken as sum a (16 + q) less (16 + z) sum a: what fp32 loses goes by sum |a S| times up to 31 and not by |a (q - z) S|, some 2^-20 of a group's
+ * sum |a S|. Where sums are not exact, a large element of A leaves that also at weights that equal their zero point. An infinity in a row of A, or a scale that is infinite, may give NaN in its row, or
+ * column. The order of the sums goes by the sizes and by whether there is scratch to split K with (there is none where a stream records the call into a graph); equal calls give equal bits. K a multiple of 32, lda a multiple of 8,
  * ldw of 16, lda below 2^23, ldw below 2^24, lds and ldz below 2^26 (MLT_ERR_UNSUPPORTED); A and Wq 16-byte, S and C 2-byte aligned. M is taken up to 64 * 65535
  * (MLT_ERR_UNSUPPORTED; any with K == 0) as far as a launch has room for its tiles of 64 rows and 128 or 256 columns; the kernels are made for up to 64 rows (the weights are read again for every 64). M == 0 or N == 0 is a no-op, K == 0 stores zeros.
  */

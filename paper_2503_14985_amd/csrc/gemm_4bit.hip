@@ -14,8 +14,9 @@
 //     order of the parts.
 // More than 32 rows: gemm_4bit_tile.hip.
 //
-// 16 x 28672 x 8192 in groups of 128 takes 28.5 us, 4.3 TB/s (one row 24.5, 4.9 TB/s; a copy of the same bytes 26), 1 x 4096 x 4096 5.6, 32 x 28672 x 8192 41. Next to memory the vector ALU is two thirds busy:
-// with weights taken apart by three operations a pair (no constants in registers) it was 33.3 us.
+// 16 x 28672 x 8192 in groups of 128 takes 28.5 us, 4.3 TB/s (one row 24.5, 4.9 TB/s; a copy of the same bytes 26), 1 x 4096 x 4096 5.6, 32 x 28672 x 8192 41. gemm_skinny.hip
+// streams as many bytes at 6.6 TB/s, so it is not memory alone: the vector ALU is two thirds busy beside the loads (with weights taken apart by three operations a pair, no constants in registers, it was 33.3 us). 17 to 32 rows
+// have twice the products, scales and corrections for a word of weights.
 #include <stdio.h>
 
 #include "gemm_4bit.h"

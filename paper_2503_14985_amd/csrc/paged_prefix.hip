@@ -10,7 +10,7 @@
 //     query l % 16 in register r, which are k slots 8 (l / 16) .. + 7 of the second product (four from each half of 16 keys): P needs no exchange between lanes, and the
 //     transposing LDS read fetches V for the same keys. P goes in as the sum of two 16-bit numbers, itself rounded and what that left (16 bits of bf16, 22 of fp16): the matrix
 //     units have time for it. Its sum is taken in fp32 before the rounding.
-// 64 sequences, 32 heads over 8, D = 128, behind a prefix of 8192 with up to 512 own keys: 35 us (29 here, of which a third is the partial results of 17 ranges; 6 in joining them); 250 behind 32001: 151 us, the
+// 64 sequences, 32 heads over 8, D = 128, behind a prefix of 8192 with up to 512 own keys: 35 us (29 here, of which a third is the partial results of 17 ranges; 6 in joining them); 250 behind 32001: 150 to 157 us, the
 // rate of the prompts' kernel; 64 behind 1024 with up to 4096 own keys: 120 us, 5.6 TB/s. Ranges of 8 key tiles at least: with 4 the first takes 53 us, with 12 35, but 16 sequences behind 4096 keys 25 instead of 21.
 // Short prefixes are not shared at all (plan_prefix). A sequence that ends inside the prefix is not part of it: all of its keys, up to its end, are its own, read through the prefix's table. So are they where there is no room for
 // partial results.

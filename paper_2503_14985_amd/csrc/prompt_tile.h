@@ -1,4 +1,4 @@
-// What the kernels of prompt.hip and prompt_ks.hip share: which item a workgroup takes, and where the rows of a sequence's queries, keys and values lie.
+// What the kernels of prompt.hip, prompt_split.hip and (prompt_body) paged_prefix.hip share: which item a workgroup takes, and where the rows of a sequence's queries, keys and values lie.
 //
 // Rows. The G = Hq / H query heads that read one key/value head are rows of one matrix: row r of sequence b and key/value head h is query head h G + r % G
 // of the sequence's token r / G. A tile of rows covers all of its tokens' heads, so that the keys are read once for all of them, and under the causal mask few tokens
@@ -334,6 +334,13 @@ __device__ __forceinline__ uint32_t prompt_redo(const PromptKernel& p, const Pro
   return redo;
 }
 
+// What a workgroup does of an item when its keys are split over several: tiles t0 .. t0 + tiles - 1 of them; the result goes, in fp32 and not divided by the sum, to
+// o[(row * parts + part) * D ...], its maximum (log2 domain) and sum to s[(row * parts + part) * 2 ...]; row: of Q, all heads counted.
+struct PromptPart {
+  int t0, tiles, part, parts;
+  float *o, *s;
+};
+
 // One item, by 8 wavefronts.
 //
 // The products, their schedule and the LDS ring are those of mha_pp.hip: workgroup = 8 wavefronts x 32 rows, key tiles of 64, S^T = K Q^T and O^T += V^T P^T on 32x32x16 MFMAs
@@ -346,18 +353,12 @@ __device__ __forceinline__ uint32_t prompt_redo(const PromptKernel& p, const Pro
 //   * A masked key's weight is 0, and 0 times a V that is not finite would be NaN. A row whose output is not finite, and to whose last tiles such a V belongs that it does not
 //     see, is worked out again by itself (prompt_redo). Nothing is spent on that before it is needed but one look at the outputs, 64 multiplications an item.
 //
-// 8192 tokens, 32 heads over 8, D = 128: 470 us, 1170 TFLOP/s (the two-group kernel for a whole batch: 1150 to 1215); 512 tokens each of four sequences behind up to 8192 keys: 212 us. What bounds it is there the board's
-// power and the exponentials beside the MFMAs, here that the longest of 272 items is as long as the call; with short sequences the start and end of an item (13 prompts of 8191 tokens in all: 92 us).
+// 8192 tokens, 32 heads over 8, D = 128: 470 to 506 us on several cards, 1090 to 1170 TFLOP/s (the two-group kernel for a whole batch: 1150 to 1215); 512 tokens each of four sequences behind up to 8192 keys: 212 to 226 us. What bounds it is there the board's
+// power and the exponentials beside the MFMAs, here that the longest of 272 items is as long as the call; with short sequences the start and end of an item, which nothing hides as a workgroup takes one item and a CU holds one
+// workgroup (13 prompts of 8191 tokens in all: 89 to 92 us).
 //
 // The largest weight of a row lies between 1 and 2^8 (the reference moves when the maximum has grown by 8): fp16 weights lose nothing but what is below 2^-25 of it. Weights are
 // rounded to 16 bits for the second product, and it is the rounded ones that are summed: what the rounding does to a row's weights as a whole cancels.
-// What a workgroup does of an item when its keys are split over several: tiles t0 .. t0 + tiles - 1 of them; the result goes, in fp32 and not divided by the sum, to
-// o[(row * parts + part) * D ...], its maximum (log2 domain) and sum to s[(row * parts + part) * 2 ...]; row: of Q, all heads counted.
-struct PromptPart {
-  int t0, tiles, part, parts;
-  float *o, *s;
-};
-
 template <typename Tag, int D, bool CAUSAL, bool PAGED, bool SPLIT>
 __device__ __forceinline__ void prompt_body(const PromptKernel& p, const PromptSeq& seq, int b, int head, int qt, uint32_t lds0, const PromptPart& part) {
   typedef PaCfg<D> L;
