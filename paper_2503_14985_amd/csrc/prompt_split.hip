@@ -30,7 +30,7 @@ __global__ __launch_bounds__(PA_NT, 1) void prompt_split_kernel(PromptKernel p, 
 
 // A wavefront a row: the parts' results, each with its own reference, on the largest one's. A row whose sequence has no such token is none and stays as it is.
 template <typename Tag, int D, bool CAUSAL, bool PAGED>
-__global__ __launch_bounds__(256) void prompt_join_kernel(PromptKernel p, const float* __restrict__ part_o, const float* __restrict__ part_s, int parts) {
+__global__ __launch_bounds__(256, 8) void prompt_join_kernel(PromptKernel p, const float* __restrict__ part_o, const float* __restrict__ part_s, int parts) {
   constexpr int E = D / 64;
   const int lane = threadIdx.x & 63, G = p.items.G, Hq = p.items.H * G;
   const int64_t q = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
@@ -77,19 +77,20 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptKernel p, const 
       }
     }
   }
-  float sum = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) sum = __builtin_fmaf(acc[e], 0.f, sum);
-  if (__any(!(sum == 0.f))) {                            // as at the end of prompt_body
-    const int row = (tok - seq.q0) * G + hq % G, last_r = seq.n * G - 1, shift = seq.m - seq.n + 1;
-    auto end_of = [&](int r) { return CAUSAL ? shift + (r < last_r ? r : last_r) / G : seq.m; };
-    const int there = end_of(row / PA_BM * PA_BM + PA_BM - 1), w_end = end_of(row / 32 * 32 + 31);
-    if (prompt_redo<Tag, D, CAUSAL, PAGED>(p, seq, b, head, row / 32 * 32, 1u << (row % 32), (w_end + PA_BN - 1) / PA_BN * PA_BN, there)) return;
-  }
   const float inv = S == 0.f ? 0.f : 1.f / S;
   uint16_t* out = p.O + (int64_t)tok * p.ldo + (int64_t)hq * D + lane * E;
 #pragma unroll
   for (int e = 0; e < E; ++e) out[e] = Elem<Tag>::from_f32(acc[e] * inv);
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) sum = __builtin_fmaf(acc[e], 0.f, sum);
+  if (__any(!(sum == 0.f)) && S - S == 0.f) {             // as at the end of prompt_body
+    const int row = (tok - seq.q0) * G + hq % G, last_r = seq.n * G - 1, shift = seq.m - seq.n + 1;
+    auto end_of = [&](int r) { return CAUSAL ? shift + (r < last_r ? r : last_r) / G : seq.m; };
+    const int there = end_of(row / PA_BM * PA_BM + PA_BM - 1), w_end = end_of(row / 32 * 32 + 31);
+    const uint32_t bit = 1u << (row % 32);
+    prompt_redo<Tag, D, CAUSAL, PAGED>(p, seq, b, head, row / 32 * 32, bit, S == 0.f ? bit : 0u, (w_end + PA_BN - 1) / PA_BN * PA_BN, there);
+  }
 }
 
 template <typename Tag, int D, bool CAUSAL, bool PAGED>

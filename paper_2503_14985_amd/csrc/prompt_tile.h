@@ -292,20 +292,47 @@ constexpr int kPromptPart = 512;                     // keys that a part of an i
 // prompt_split.hip: `parts` workgroups to an item; scratch: T * Hq * parts * (D + 2) numbers
 int run_prompt_split(const PromptKernel& p, int dtype, int D, int64_t grid, int parts, float* scratch, hipStream_t s);
 
-// exponent all ones: a number that is not finite
+// What a number that is not finite is, in bits: 1 +inf, 2 -inf, 4 NaN; 0 for a finite one
 template <typename Tag>
-__device__ __forceinline__ bool wild(uint32_t pair, int half) {
-  constexpr uint32_t E = __is_same(Tag, bf16_tag) ? 0x7f80u : 0x7c00u;
-  return ((pair >> (16 * half)) & E) == E;
+__device__ __forceinline__ uint32_t wild(uint16_t x) {
+  constexpr uint32_t INF = __is_same(Tag, bf16_tag) ? 0x7f80u : 0x7c00u;
+  const uint32_t a = x & 0x7fffu;
+  return a < INF ? 0u : a > INF ? 4u : x >> 15 ? 2u : 1u;
 }
+// ... of values of both signs among what a sum has: NaN
+__device__ __forceinline__ bool wild_nan(uint32_t w) { return w >= 3; }
 
-// By one wavefront, for rows q0 + r of its 32 whose outputs are not finite (bits r of `bad`): where a value that is not finite was among those that its tiles hold (up to key
-// `held`; those from `there` on are key there - 1 again) and that the row does not see, the row is worked out again from the keys that it sees, one after the other
-// (attn_rows.h), and stored. Returns the bits of those rows. (An accident of one token costs the rows around it that, and no others.)
+// By one wavefront, after its rows have been stored: for rows q0 + r of its 32 whose outputs are not finite though the sums of their weights are (bits r of `bad`; of `none`: that sum is 0). The
+// tiles hold keys up to `held`; those from `there` on are key there - 1 again. Where values that a row does not see are not finite, their weight of 0 has made NaN of the output's elements. Such an
+// element is an infinity or NaN all the same if the row sees one there itself, which is found by looking at the values alone, one key after the other, once for all 32 rows (a row sees what
+// the rows before it see). Otherwise the row is worked out again from the keys that it sees (attn_rows.h); these are rows in front of the first such value of an element, 64 tokens of each at most.
 template <typename Tag, int D, bool CAUSAL, bool PAGED>
-__device__ __forceinline__ uint32_t prompt_redo(const PromptKernel& p, const PromptSeq& seq, int b, int head, int q0, uint32_t bad, int held, int there) {
+__device__ __forceinline__ void prompt_redo(const PromptKernel& p, const PromptSeq& seq, int b, int head, int q0, uint32_t bad, uint32_t none, int held, int there) {
+  constexpr int E = D / 64;
   const int lane = threadIdx.x & 63, G = p.items.G, rows = seq.n * G;
-  uint32_t redo = 0;
+  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");       // what is stored here comes after what has been stored
+  auto look = [&](int from, int to, uint32_t (&w)[E]) __attribute__((always_inline)) {   // elements 64 e + lane of values from .. to - 1
+#pragma clang loop unroll(disable)
+    for (int k0 = from; k0 < to; k0 += 8) {
+      uint16_t x[8][E];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const uint16_t* v = prompt_value<D, PAGED>(p.src, seq, b, p.items.H, head, k0 + k < to ? k0 + k : to - 1);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[k][e] = v[64 * e + lane];
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) w[e] |= wild<Tag>(x[k][e]);
+      bool all = true;
+#pragma unroll
+      for (int e = 0; e < E; ++e) all = all && wild_nan(w[e]);
+      if (__all(all)) break;                               // (it gets no worse)
+    }
+  };
+  uint32_t seen[E] = {};
+  int upto = 0;                                            // keys that `seen` has
 #pragma clang loop unroll(disable)
   while (bad) {
     const int r = __builtin_ctz(bad);
@@ -313,25 +340,30 @@ __device__ __forceinline__ uint32_t prompt_redo(const PromptKernel& p, const Pro
     if (q0 + r >= rows) break;
     const int tok = uniform((q0 + r) / G), g = q0 + r - tok * G, end = CAUSAL ? seq.m - seq.n + 1 + tok : seq.m;
     const int last = held < there ? held : there, first = held > there && end > there - 1 ? there - 1 : end;
-    bool found = false;
-#pragma clang loop unroll(disable)
-    for (int key = (first > 0 ? first : 0) + lane; key < last; key += 64) {
-      const uint16_t* v = prompt_value<D, PAGED>(p.src, seq, b, p.items.H, head, key);
-#pragma clang loop unroll(disable)
-      for (int d = 0; d < D; d += 2) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(v + d);
-        found |= wild<Tag>(w, 0) || wild<Tag>(w, 1);
-      }
+    uint32_t unseen[E] = {};
+    look(first > 0 ? first : 0, last, unseen);
+    bool some = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e) some = some || unseen[e];
+    if (!__any(some)) continue;
+    if (end > upto) {
+      look(upto, end, seen);
+      upto = end;
     }
-    if (!__any(found)) continue;
-    redo |= 1u << r;
+    bool again = none >> r & 1;
+#pragma unroll
+    for (int e = 0; e < E; ++e) again = again || (unseen[e] && !seen[e]);
     const int64_t at = (int64_t)(head * G + g) * D;
-    const uint16_t* q = p.Q + (int64_t)(seq.q0 + tok) * p.ldq + at;
-    const float c = p.negate ? -p.c : p.c;
-    attend_row<Tag, D>(q, p.O + (int64_t)(seq.q0 + tok) * p.ldo + at, end, [&](int64_t j) { return prompt_key<D, PAGED>(p.src, seq, b, p.items.H, head, (int)j); },
-                       [&](int64_t j) { return prompt_value<D, PAGED>(p.src, seq, b, p.items.H, head, (int)j); }, c);
+    uint16_t* out = p.O + (int64_t)(seq.q0 + tok) * p.ldo + at;
+    if (__any(again)) {
+      attend_row<Tag, D>(p.Q + (int64_t)(seq.q0 + tok) * p.ldq + at, out, end, [&](int64_t j) { return prompt_key<D, PAGED>(p.src, seq, b, p.items.H, head, (int)j); },
+                         [&](int64_t j) { return prompt_value<D, PAGED>(p.src, seq, b, p.items.H, head, (int)j); }, p.negate ? -p.c : p.c);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (unseen[e]) out[64 * e + lane] = Elem<Tag>::from_f32(wild_nan(seen[e]) ? __builtin_nanf("") : seen[e] == 2 ? -__builtin_inff() : __builtin_inff());
+    }
   }
-  return redo;
 }
 
 // What a workgroup does of an item when its keys are split over several: tiles t0 .. t0 + tiles - 1 of them; the result goes, in fp32 and not divided by the sum, to
@@ -351,7 +383,7 @@ struct PromptPart {
 //     number for each tile, read by the scalar unit a tile ahead.
 //   * A row may see no key at all: weights are taken against 0 while the maximum is -inf, and a sum of 0 gives an output of 0.
 //   * A masked key's weight is 0, and 0 times a V that is not finite would be NaN. A row whose output is not finite, and to whose last tiles such a V belongs that it does not
-//     see, is worked out again by itself (prompt_redo). Nothing is spent on that before it is needed but one look at the outputs, 64 multiplications an item.
+//     see, is put right afterwards (prompt_redo). Nothing is spent on that before it is needed but one look at the outputs, 64 multiplications an item.
 //
 // 8192 tokens, 32 heads over 8, D = 128: 470 to 506 us on several cards, 1090 to 1170 TFLOP/s (the two-group kernel for a whole batch: 1150 to 1215); 512 tokens each of four sequences behind up to 8192 keys: 212 to 226 us. What bounds it is there the board's
 // power and the exponentials beside the MFMAs, here that the longest of 272 items is as long as the call; with short sequences the start and end of an item, which nothing hides as a workgroup takes one item and a CU holds one
@@ -663,15 +695,13 @@ __device__ __forceinline__ void prompt_body(const PromptKernel& p, const PromptS
     return;
   }
 
-  // ---- rows to be done again: an output is not finite, and so is a value that the row's last tiles hold without its seeing it
+  // ---- rows to be looked at again (prompt_redo): an output is not finite, though the sum of the weights is
   float sum = 0.f;                          // x * 0 is 0, or NaN where x is not finite
 #pragma unroll
   for (int t = 0; t < NDT; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) sum = __builtin_fmaf(o_acc[t][r], 0.f, sum);
-  const uint64_t bad = __builtin_amdgcn_ballot_w64(!(sum == 0.f));
-  uint32_t redo = 0;
-  if (bad) redo = prompt_redo<Tag, D, CAUSAL, PAGED>(p, seq, b, head, q0, (uint32_t)bad | (uint32_t)(bad >> 32), my_nblk * PA_BN, wg_end);
+  const uint64_t bad = __builtin_amdgcn_ballot_w64(!(sum == 0.f) && l_tot - l_tot == 0.f), none = __builtin_amdgcn_ballot_w64(l_tot == 0.f);
 
   // ---- epilogue: O = O^T / l, l summed over both key halves, rows without keys 0; whole rows through LDS, 16 bytes a lane
   const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
@@ -701,8 +731,9 @@ __device__ __forceinline__ void prompt_body(const PromptKernel& p, const PromptS
     const int r = i * L::RPB + lane / L::CPR, cc = lane % L::CPR;
     const u32x4 v = *(const MLT_LDS u32x4*)(uintptr_t)(o_lds + r * ROWB + ((cc ^ (r & CM)) << 4));
     const int piece = __shfl(o_piece, r);
-    if (q0 + r < rows && !(redo >> r & 1)) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_mem*>(ob + ((int64_t)piece + cc) * 8));
+    if (q0 + r < rows) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_mem*>(ob + ((int64_t)piece + cc) * 8));
   }
+  if (bad) prompt_redo<Tag, D, CAUSAL, PAGED>(p, seq, b, head, q0, (uint32_t)bad | (uint32_t)(bad >> 32), (uint32_t)none, my_nblk * PA_BN, wg_end);
 }
 
 }  // namespace mlt
